@@ -207,7 +207,7 @@ def _plain_logprobs_backward(s):
 
 
 def _distill_rows(s, dtype):
-    """(loss, what the gradient takes from the loss) in `dtype`, and the log probabilities of the listed tokens."""
+    """(loss, what the gradient takes from the loss); the vocabulary's sums in `dtype`."""
     z, t, temperature, tail = s["logits"].to(dtype), s["teacher_logprob"].double(), s["temperature"], s["tail"]
     n, vocab = z.shape
     idx = s["teacher_idx"].long()
@@ -228,14 +228,15 @@ def _distill_rows(s, dtype):
         left = (1.0 - q.sum(1, keepdim=True)).clamp(min=0.0)
         loss = loss + torch.where(left > 0, left * (left.log() - log_rest), 0.0)[:, 0]
         mass = q.sum(1, keepdim=True) + left
-        factor = mass - left / log_rest.exp()
+        log_ratio = left.log() - log_rest
     else:
-        mass = factor = q.sum(1, keepdim=True)
-    return loss, torch.cat([m.double(), log_sum, norm, mass, factor], 1), q, valid
+        mass = q.sum(1, keepdim=True)
+        log_ratio = torch.full_like(mass, -math.inf)
+    return loss, torch.cat([m.double(), log_sum, norm, mass, log_ratio], 1)
 
 
 def _plain_distill(s):
-    loss, stats, _, _ = _distill_rows(s, torch.float32)
+    loss, stats = _distill_rows(s, torch.float32)
     return dict(loss=loss.float(), stats=stats.float())
 
 
@@ -245,13 +246,13 @@ def _plain_distill_backward(s, stats):
     idx = s["teacher_idx"].long()
     valid = (idx >= 0) & (idx < vocab)
     at = idx.clamp(0, vocab - 1)
-    m, log_sum, norm, mass, factor = (stats[:, i:i + 1] for i in range(5))
+    m, log_sum, norm, mass, log_ratio = (stats[:, i:i + 1] for i in range(5))
     g = s["grad_loss"][:, None] / temperature
     p = ((z - m) / temperature - log_sum).exp()
     t = s["teacher_logprob"] if s["tail"] else s["teacher_logprob"] / temperature - norm
     q = t.exp().masked_fill(~valid, 0.0)
     here = (mass * p.gather(1, at) - q).masked_fill(~valid, 0.0)
-    grad = torch.cat([p * factor, torch.zeros_like(g)], 1)  # a column for the entries that name no token
+    grad = torch.cat([p * (mass - log_ratio.exp()), torch.zeros_like(g)], 1)  # a column for the entries that name no token
     grad.scatter_(1, torch.where(valid, at, vocab), here)
     return (g * grad[:, :vocab]).to(s["logits"].dtype)
 
@@ -382,14 +383,14 @@ def exact(case, seed):
     dense, inside = dense[:, :vocab], inside[:, :vocab]
     p = logp.exp()
     loss = torch.where(dense > 0, dense * (dense.log() - logp), 0.0).sum(1)
-    mass, per_unlisted = q.sum(1), torch.zeros(case["n"], dtype=torch.float64, device="cuda")
+    mass, per_unlisted = q.sum(1), torch.zeros(case["n"], dtype=torch.float64, device="cuda")  # an unlisted token's p has mass - per_unlisted
     if case["tail"]:
         q_rest = (1 - q.sum(1)).clamp(min=0)
         p_rest = torch.where(inside, 0.0, p).sum(1)
         loss = loss + torch.special.xlogy(q_rest, q_rest) - torch.special.xlogy(q_rest, p_rest)
         mass, per_unlisted = mass + q_rest, q_rest / p_rest
     norm = torch.zeros_like(mass) if case["tail"] else torch.logsumexp((t / case["temperature"]).masked_fill(~valid, -math.inf), 1)
-    out = {"loss": loss, "stats": torch.stack([m, lse - m / case["temperature"], norm, mass, mass - per_unlisted], 1)}
+    out = {"loss": loss, "stats": torch.stack([m, lse - m / case["temperature"], norm, mass, per_unlisted.log()], 1)}
     if case["direction"] == "forward":
         return out
     grad = mass[:, None] * p - dense - torch.where(inside, 0.0, p * per_unlisted[:, None])
