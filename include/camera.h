@@ -22,9 +22,11 @@
  *   - The context owns a grow-only device workspace (hipMalloc on first use and
  *     on growth, which synchronises the device) and, for the ranking calls, a
  *     small persistent selection state made on their first use.
- *   - NaN / Inf in the inputs: results unspecified (not checked).
+ *   - NaN / Inf in the inputs: results unspecified (not checked).  (The calls on
+ *     logits say what -Inf means there.)
  *   - Device data pointers must be 16-byte aligned; for CAMERA_BF16 d_model and
- *     ldx must be multiples of 8, for CAMERA_F32 multiples of 4.
+ *     ldx must be multiples of 8, for CAMERA_F32 multiples of 4.  (The calls on
+ *     logits take rows that start at any element.)
  */
 #ifndef CAMERA_H_
 #define CAMERA_H_
@@ -51,13 +53,16 @@ enum camera_dtype { CAMERA_F32 = 0, CAMERA_BF16 = 1 };
 
 enum camera_flags {
   CAMERA_ACCUMULATE = 1, /* phi2 / phi_inf already hold earlier token chunks: merge into them */
-  CAMERA_NO_FINALIZE = 2 /* more chunks follow: leave omega2 and energy untouched */
+  CAMERA_NO_FINALIZE = 2, /* more chunks follow: leave omega2 and energy untouched */
+  CAMERA_DISTILL_TAIL = 4 /* camera_distill_topk: the tokens that the teacher does not list are one more class */
 };
 
 /* Limits of this build. */
 #define CAMERA_MAX_EXPERTS 256   /* routed experts per call */
 #define CAMERA_MAX_SEGMENTS 512  /* expert segments in select / alloc */
 #define CAMERA_MAX_LEVELS 8      /* precision classes in camera_alloc_bits */
+#define CAMERA_MAX_ALTERNATIVES 256 /* tokens a position in camera_token_logprobs (top_k) and camera_distill_topk (k) */
+#define CAMERA_DISTILL_STATS 5   /* floats a position that camera_distill_topk leaves for its gradient */
 #define CAMERA_MAX_ROW_ALIGN 512 /* largest row alignment (elements) of the compacted W_down blocks */
 
 /* Kernel groups for camera_profile_read. */
@@ -73,7 +78,10 @@ enum camera_kernel_id {
   CAMERA_K_COMBINE = 8,  /* camera_layer_forward: sum over a token's experts; camera_output_error */
   CAMERA_K_COMPACT_HIDDEN = 9, /* camera_layer_forward_compact: Lambda on the kept gate / up rows */
   CAMERA_K_COMPACT_DOWN = 10,  /* camera_layer_forward_compact: Lambda times the kept W_down columns */
-  CAMERA_K_COUNT = 11
+  CAMERA_K_LOGPROBS = 11,      /* camera_token_logprobs and its gradient */
+  CAMERA_K_DISTILL = 12,       /* camera_distill_topk and its gradient */
+  CAMERA_K_GATED_GRAD = 13,    /* camera_gated_ffn_backward: dG, dU and the transposed operands of its products */
+  CAMERA_K_COUNT = 14
 };
 
 /* Create / destroy a context bound to HIP device `device`.  Creation touches no
@@ -372,6 +380,110 @@ int camera_layer_forward_compact(camera_ctx* ctx, void* stream,
                                  int flags, float* Y);
 int camera_output_error(camera_ctx* ctx, void* stream, const float* Y, const float* Y_hat,
                         int64_t n, int64_t d_model, float* per_token);
+
+/*
+ * What a pruned model says of given tokens.  With z = a row of logits, p = softmax(z / temperature):
+ *   logprob[i]     = log p_t for the row's target t
+ *   entropy[i]     = - sum over v of p_v log p_v
+ *   stats[i]       = max z, log sum exp((z - max z) / temperature)          (what the gradient takes)
+ *   top_idx[i][j]  = the token with the j-th largest logit, equal logits to the lower index (-0 equals +0);
+ *   top_logprob    = its log p.  An alternative without probability (logit -Inf) has index -1 and log p -Inf.
+ *
+ *   logits   [n x vocab], row stride ld >= vocab elements, `dtype`; rows may start at any element.  A logit of -Inf rules a
+ *            token out.  A row that rules every token out: entropy 0, stats -Inf and 0, logprob -Inf.  NaN or +Inf in a row:
+ *            that row's results are unspecified (its indices are tokens or -1).
+ *   temperature  > 0, finite
+ *   targets  int32 [n]; a value outside [0, vocab) stands for a position without target: logprob 0.  NULL with logprob NULL.
+ *   top_k    in [0, min(vocab, CAMERA_MAX_ALTERNATIVES)]; 0: top_idx and top_logprob are not written (may be NULL)
+ *   logprob, entropy float32 [n], stats float32 [n x 2], top_idx int32 [n x top_k], top_logprob float32 [n x top_k] out; each of
+ *            the first three may be NULL
+ * Sums are taken in float32, in an order that depends on n, vocab and dtype only.  The workspace of a call serves every call with
+ * the same or a smaller top_k, whatever n and vocab.  n == 0 does nothing.
+ *
+ * camera_token_logprobs_backward: the gradient with respect to the logits of
+ *   sum over i of grad_logprob[i] logprob[i] + grad_entropy[i] entropy[i]
+ *   stats, entropy   as the forward call left them for the same logits and temperature
+ *   grad_logprob     float32 [n], or NULL: 0.  Ignored where the position has no target.
+ *   grad_entropy     float32 [n], or NULL: 0 (entropy may then be NULL too).  Not both NULL.
+ *   flags            0, or CAMERA_ACCUMULATE: the gradient is added to what dlogits holds
+ *   dlogits          [n x vocab], row stride ldd >= vocab, `dtype`, out (elements behind a row's end are left alone).  Without
+ *            CAMERA_ACCUMULATE it may be `logits` itself (ldd == ld then); any other overlap is not allowed.
+ * Each value is computed in float32 and rounded once to `dtype` (with CAMERA_ACCUMULATE after the addition).  Rows without gradient
+ * (both factors 0) are set to 0 without reading their logits; so are rows that rule every token out.
+ */
+int camera_token_logprobs(camera_ctx* ctx, void* stream,
+                          const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
+                          const int32_t* targets, int top_k,
+                          float* logprob, float* entropy, float* stats, int32_t* top_idx, float* top_logprob);
+int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
+                                   const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
+                                   const int32_t* targets, const float* stats, const float* entropy,
+                                   const float* grad_logprob, const float* grad_entropy, int flags,
+                                   void* dlogits, int64_t ldd);
+
+/*
+ * How far the pruned model's distribution is from the original model's, of which the k most likely tokens of every position
+ * are known (top_idx and top_logprob of camera_token_logprobs on its logits): the Kullback-Leibler divergence
+ *   loss[i] = sum over the listed tokens j of q_j (log q_j - log p_j)
+ * with p = softmax(logits / temperature) over the whole vocabulary and q the teacher's distribution:
+ *   flags 0                    q = softmax(teacher_logprob / temperature) over the row's entries (logits do as well there)
+ *   flags CAMERA_DISTILL_TAIL  q_j = exp(teacher_logprob_j), which were taken at this temperature, and all tokens that are not
+ *            listed are one more class: + q_r (log q_r - log p_r), q_r = max(0, 1 - sum q_j), p_r = the sum of their p.  Where no
+ *            token is left for it the class drops out.
+ *   logits, temperature   as in camera_token_logprobs
+ *   teacher_idx      int32 [n x k]; an entry outside [0, vocab) is ignored, and so is one that repeats an earlier entry of its row
+ *   teacher_logprob  float32 [n x k]; an entry of -Inf is ignored.  1 <= k <= CAMERA_MAX_ALTERNATIVES.
+ *   loss   float32 [n] out.  A row without entries has loss 0 (with CAMERA_DISTILL_TAIL: all of its probability is in the one
+ *            class, loss 0).  +Inf where a listed token with q_j > 0 has logit -Inf.
+ *   stats  float32 [n x CAMERA_DISTILL_STATS] out, for the gradient: max of the logits, log sum exp((z - max) / temperature),
+ *            log sum exp(teacher_logprob / temperature) (0 with CAMERA_DISTILL_TAIL), the sum of q, and log(q_r / p_r) (-Inf
+ *            without that class): an unlisted token's part of the gradient is p (sum of q - q_r / p_r)
+ * The vocabulary's sums are taken in float32, those over the listed tokens in float64.  n == 0 does nothing.
+ *
+ * camera_distill_topk_backward: the gradient with respect to the logits of the sum over i of grad_loss[i] loss[i]; stats, flags
+ * (with CAMERA_ACCUMULATE allowed) and dlogits as above, the same teacher, temperature and CAMERA_DISTILL_TAIL as in the forward
+ * call.  Rows with grad_loss 0 are set to 0 without reading their logits.
+ */
+int camera_distill_topk(camera_ctx* ctx, void* stream,
+                        const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
+                        const int32_t* teacher_idx, const float* teacher_logprob, int k, int flags,
+                        float* loss, float* stats);
+int camera_distill_topk_backward(camera_ctx* ctx, void* stream,
+                                 const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
+                                 const int32_t* teacher_idx, const float* teacher_logprob, int k,
+                                 const float* stats, const float* grad_loss, int flags,
+                                 void* dlogits, int64_t ldd);
+
+/*
+ * The gated block of a feed-forward layer, for the micro-experts of one expert (all of them, or those that
+ * camera_gather_micro_experts packed: its rows of W_gate_out and W_up_out):
+ *   H[j, c] = silu(<w_gate_c, x_j>) <w_up_c, x_j>
+ *   X       [n x d_model], row stride ldx, `dtype`
+ *   W_gate, W_up  [d_ff x d_model] `dtype`, rows contiguous; d_ff any positive number
+ *   H       [n x d_ff] `dtype` out, or NULL; row stride ldh, a multiple of 8 (CAMERA_BF16) or 4 (CAMERA_F32) and at least d_ff.
+ *           Columns d_ff .. the next multiple are written as zeros, those behind it left alone.
+ *   pre     float32 [n x 2 x P] out, or NULL; P = d_ff rounded up to a multiple of 8: the two projections of every token (first
+ *           gate, then up), which the backward call takes.  Columns from d_ff on are unspecified.
+ * Both products are accumulated in float32 and H is rounded once.  Which kernel runs depends on n, so a token's last bits may.
+ *
+ * camera_gated_ffn_backward: from dH = the gradient with respect to H,
+ *   dU = dH silu(G),  dG = dH U silu'(G),  dX = dG W_gate + dU W_up,  dW_gate = dG^T X,  dW_up = dU^T X
+ *   pre     what the forward call left for the same X, W_gate, W_up, or NULL: the projections are computed again
+ *   dH      [n x d_ff] `dtype`, row stride lddh >= d_ff; rows may start at any element
+ *   dX      [n x d_model] out, row stride lddx, a multiple of 8 (4) elements;  dW_gate, dW_up  [d_ff x d_model] out, rows
+ *           contiguous; all of `dtype`.  Each may be NULL (not computed).
+ * With CAMERA_BF16 dG and dU are rounded to bf16 before the products (operands of the matrix instructions), which accumulate in
+ * float32 and round their result once.  n == 0 sets dW_gate and dW_up to zero.  No output may overlap an input.
+ */
+int camera_gated_ffn(camera_ctx* ctx, void* stream,
+                     const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
+                     const void* W_gate, const void* W_up, int64_t d_ff,
+                     void* H, int64_t ldh, float* pre);
+int camera_gated_ffn_backward(camera_ctx* ctx, void* stream,
+                              const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
+                              const void* W_gate, const void* W_up, int64_t d_ff,
+                              const float* pre, const void* dH, int64_t lddh,
+                              void* dX, int64_t lddx, void* dW_gate, void* dW_up);
 
 /*
  * Per-kernel-group timing for benchmarks.  With profiling on, every launch

@@ -16,15 +16,17 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libcamera_hip.so")
 
 F32, BF16 = 0, 1
-ACCUMULATE, NO_FINALIZE = 1, 2
+ACCUMULATE, NO_FINALIZE, DISTILL_TAIL = 1, 2, 4
+MAX_ALTERNATIVES, DISTILL_STATS = 256, 5
 K_ROUTE, K_BUCKET, K_GEMM, K_DOWN_NORM, K_FINALIZE, K_RANK, K_GATHER, K_DOWN_GEMM, K_COMBINE = range(9)
 KERNEL_NAMES = ["route", "bucket", "gemm", "down_norm", "finalize", "rank", "gather", "down_gemm", "combine",
-                "compact_hidden", "compact_down"]
+                "compact_hidden", "compact_down", "logprobs", "distill", "gated_grad"]
 
 EXPORTS = ["camera_create", "camera_destroy", "camera_last_error", "camera_version", "camera_route_topk",
            "camera_score_layer", "camera_select_prune", "camera_select_prune_noalloc", "camera_select_prune_multi", "camera_alloc_bits", "camera_rank_decisions",
-           "camera_gather_micro_experts", "camera_input_channel_energy", "camera_layer_forward", "camera_layer_forward_compact", "camera_output_error", "camera_profile_enable",
-           "camera_profile_read"]
+           "camera_gather_micro_experts", "camera_input_channel_energy", "camera_layer_forward", "camera_layer_forward_compact", "camera_output_error",
+           "camera_token_logprobs", "camera_token_logprobs_backward", "camera_distill_topk", "camera_distill_topk_backward",
+           "camera_gated_ffn", "camera_gated_ffn_backward", "camera_profile_enable", "camera_profile_read"]
 
 _c = ctypes
 _vp, _i, _i64, _f, _d = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_float, _c.c_double
@@ -65,6 +67,12 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.camera_layer_forward_compact.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i, _i, _i,
                                                  _c.POINTER(_c.c_int32), _i, _vp, _vp, _vp, _i, _vp]
     lib.camera_output_error.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _vp]
+    lib.camera_token_logprobs.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _f, _vp, _i, _vp, _vp, _vp, _vp, _vp]
+    lib.camera_token_logprobs_backward.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i64]
+    lib.camera_distill_topk.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _i, _vp, _vp]
+    lib.camera_distill_topk_backward.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _f, _vp, _vp, _i, _vp, _vp, _i, _vp, _i64]
+    lib.camera_gated_ffn.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp]
+    lib.camera_gated_ffn_backward.argtypes = [_vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp]
     lib.camera_profile_enable.argtypes = [_vp, _i]
     lib.camera_profile_read.argtypes = [_vp, _i, _c.POINTER(_d), _c.POINTER(_i64)]
     for name in EXPORTS:
@@ -118,6 +126,11 @@ def _check_flat(t, name: str, dtype=None, device=None):
         _require(t.dtype == dtype, f"{name}: must be {dtype}")
     if device is not None:
         _require(t.device == device, f"{name}: on another device")
+
+
+def _row_stride(t) -> int:
+    """Elements between rows; a matrix of at most one row has none of its own (torch leaves any value there)."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
 
 
 def _stream_handle(device) -> _vp:
@@ -368,6 +381,135 @@ class Camera:
         self._check(self.lib.camera_output_error(self._ctx, _stream_handle(self.device), _ptr(Y), _ptr(Y_hat), n, d,
                                                  _ptr(out)))
         return out
+
+    # ---- judging and repairing a pruned model ------------------------------
+    @staticmethod
+    def _check_logits(logits, per_row=()):
+        """Logits as a matrix, and float32 / int32 tensors with a value (or a fixed number of values) for every row of it."""
+        _check_matrix(logits, "logits")
+        for t, name, dtype, shape in per_row:
+            if t is None:
+                continue
+            _check_flat(t, name, dtype, logits.device)
+            _require(tuple(t.shape) == shape, f"{name}: must be {list(shape)} (got {list(t.shape)})")
+
+    def _gradient_rows(self, logits, dlogits, accumulate):
+        if dlogits is None:
+            _require(not accumulate, "accumulate: needs dlogits")
+            return torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
+        _check_matrix(dlogits, "dlogits", like=logits)
+        _require(dlogits.shape == logits.shape, "dlogits: shape differs from logits")
+        return dlogits
+
+    def token_logprobs(self, logits, targets=None, top_k: int = 0, temperature: float = 1.0):
+        """Log probabilities of given tokens: logits [n, vocab] (bf16 / f32, unit inner stride, any row stride), targets int32 [n]
+        (outside [0, vocab): no target there, log probability 0) or None.  Returns dict(logprob [n], entropy [n], stats [n, 2]) and,
+        with top_k > 0, top_idx int32 [n, top_k] / top_logprob [n, top_k]: the most likely tokens, equal logits to the lower index,
+        -1 where a masked row has fewer.  `logprob` is missing without targets; `stats` is what the backward call takes."""
+        n = logits.shape[0]
+        self._check_logits(logits, [(targets, "targets", torch.int32, (n,))])
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.device)  # noqa: E731
+        out = {} if targets is None else {"logprob": new(n)}
+        out.update(entropy=new(n), stats=new(n, 2))
+        if top_k > 0:
+            out.update(top_idx=new(n, top_k, dtype=torch.int32), top_logprob=new(n, top_k))
+        self._check(self.lib.camera_token_logprobs(
+            self._ctx, _stream_handle(self.device), _ptr(logits), _dtype_code(logits), n, logits.shape[1], _row_stride(logits),
+            float(temperature), _ptr(targets), int(top_k), _ptr(out.get("logprob")), _ptr(out["entropy"]), _ptr(out["stats"]),
+            _ptr(out.get("top_idx")), _ptr(out.get("top_logprob"))))
+        return out
+
+    def token_logprobs_backward(self, logits, targets, stats, grad_logprob=None, entropy=None, grad_entropy=None,
+                                temperature: float = 1.0, dlogits=None, accumulate=False):
+        """Gradient with respect to the logits of sum(grad_logprob * logprob) + sum(grad_entropy * entropy); stats and entropy as
+        token_logprobs left them.  dlogits: written there (accumulate: added to it); it may be `logits` itself."""
+        n = logits.shape[0]
+        f32 = torch.float32
+        self._check_logits(logits, [(targets, "targets", torch.int32, (n,)), (stats, "stats", f32, (n, 2)),
+                                    (grad_logprob, "grad_logprob", f32, (n,)), (entropy, "entropy", f32, (n,)),
+                                    (grad_entropy, "grad_entropy", f32, (n,))])
+        dlogits = self._gradient_rows(logits, dlogits, accumulate)
+        self._check(self.lib.camera_token_logprobs_backward(
+            self._ctx, _stream_handle(self.device), _ptr(logits), _dtype_code(logits), n, logits.shape[1], _row_stride(logits),
+            float(temperature), _ptr(targets), _ptr(stats), _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy),
+            ACCUMULATE if accumulate else 0, _ptr(dlogits), _row_stride(dlogits)))
+        return dlogits
+
+    def distill_topk(self, logits, teacher_idx, teacher_logprob, temperature: float = 1.0, tail=False):
+        """Kullback-Leibler divergence of softmax(logits / temperature) from a teacher of which the most likely tokens are known:
+        teacher_idx int32 [n, k], teacher_logprob [n, k] (top_idx and top_logprob of token_logprobs on the teacher's logits).
+        tail: the tokens that the teacher does not list are one more class (teacher_logprob taken at this temperature); else the
+        teacher's distribution is renormalised over the listed ones.  Returns dict(loss [n], stats [n, 5])."""
+        n = logits.shape[0]
+        k = teacher_idx.shape[1]
+        self._check_logits(logits, [(teacher_idx, "teacher_idx", torch.int32, (n, k)),
+                                    (teacher_logprob, "teacher_logprob", torch.float32, (n, k))])
+        out = {"loss": torch.empty(n, dtype=torch.float32, device=self.device),
+               "stats": torch.empty((n, DISTILL_STATS), dtype=torch.float32, device=self.device)}
+        self._check(self.lib.camera_distill_topk(
+            self._ctx, _stream_handle(self.device), _ptr(logits), _dtype_code(logits), n, logits.shape[1], _row_stride(logits),
+            float(temperature), _ptr(teacher_idx), _ptr(teacher_logprob), k, DISTILL_TAIL if tail else 0, _ptr(out["loss"]),
+            _ptr(out["stats"])))
+        return out
+
+    def distill_topk_backward(self, logits, teacher_idx, teacher_logprob, stats, grad_loss, temperature: float = 1.0, tail=False,
+                              dlogits=None, accumulate=False):
+        """Gradient with respect to the logits of sum(grad_loss * loss); stats as distill_topk left them, the other arguments as it
+        had them.  dlogits: written there (accumulate: added to it); it may be `logits` itself."""
+        n = logits.shape[0]
+        k = teacher_idx.shape[1]
+        self._check_logits(logits, [(teacher_idx, "teacher_idx", torch.int32, (n, k)),
+                                    (teacher_logprob, "teacher_logprob", torch.float32, (n, k)),
+                                    (stats, "stats", torch.float32, (n, DISTILL_STATS)), (grad_loss, "grad_loss", torch.float32, (n,))])
+        dlogits = self._gradient_rows(logits, dlogits, accumulate)
+        self._check(self.lib.camera_distill_topk_backward(
+            self._ctx, _stream_handle(self.device), _ptr(logits), _dtype_code(logits), n, logits.shape[1], _row_stride(logits),
+            float(temperature), _ptr(teacher_idx), _ptr(teacher_logprob), k, _ptr(stats), _ptr(grad_loss),
+            (ACCUMULATE if accumulate else 0) | (DISTILL_TAIL if tail else 0), _ptr(dlogits), _row_stride(dlogits)))
+        return dlogits
+
+    @staticmethod
+    def _check_gated(X, W_gate, W_up):
+        _check_matrix(X, "X")
+        for t, name in ((W_gate, "W_gate"), (W_up, "W_up")):
+            _check_matrix(t, name, like=X)
+            _check_flat(t, name)
+            _require(t.shape[1] == X.shape[1], f"{name}: d_model differs from X")
+        _require(W_gate.shape == W_up.shape, "W_gate / W_up: shapes differ")
+
+    def gated_ffn(self, X, W_gate, W_up, want_pre=False, H=None):
+        """H [n, d_ff] = silu(X W_gate^T) * (X W_up^T) for the micro-experts of one expert: X [n, d_model], W_gate, W_up
+        [d_ff, d_model].  want_pre: returns (H, pre), pre [n, 2, P] float32 the two projections that the backward call takes.
+        H allocated here has rows of a whole number of 16-byte vectors (a view of the first d_ff columns)."""
+        self._check_gated(X, W_gate, W_up)
+        n, d_ff = X.shape[0], W_gate.shape[0]
+        v = 16 // X.element_size()
+        if H is None:
+            H = torch.empty((n, (d_ff + v - 1) // v * v), dtype=X.dtype, device=self.device)[:, :d_ff]
+        _check_matrix(H, "H", like=X)
+        _require(tuple(H.shape) == (n, d_ff), "H: must be [n, d_ff]")
+        pre = torch.empty((n, 2, (d_ff + 7) // 8 * 8), dtype=torch.float32, device=self.device) if want_pre else None
+        self._check(self.lib.camera_gated_ffn(
+            self._ctx, _stream_handle(self.device), _ptr(X), _dtype_code(X), n, X.shape[1], _row_stride(X), _ptr(W_gate), _ptr(W_up),
+            d_ff, _ptr(H), _row_stride(H), _ptr(pre)))
+        return (H, pre) if want_pre else H
+
+    def gated_ffn_backward(self, X, W_gate, W_up, dH, pre=None, want=(True, True, True)):
+        """(dX, dW_gate, dW_up) from dH [n, d_ff]; pre as gated_ffn left it, or None: the projections are computed again.  want:
+        which of the three (None in the place of the others)."""
+        self._check_gated(X, W_gate, W_up)
+        n, d_ff = X.shape[0], W_gate.shape[0]
+        _check_matrix(dH, "dH", like=X)
+        _require(tuple(dH.shape) == (n, d_ff), "dH: must be [n, d_ff]")
+        if pre is not None:
+            _check_flat(pre, "pre", torch.float32, X.device)
+            _require(tuple(pre.shape) == (n, 2, (d_ff + 7) // 8 * 8), "pre: must be as gated_ffn returned it")
+        new = lambda like, wanted: torch.empty(like.shape, dtype=X.dtype, device=self.device) if wanted else None  # noqa: E731
+        dX, dW_gate, dW_up = new(X, want[0]), new(W_gate, want[1]), new(W_up, want[2])
+        self._check(self.lib.camera_gated_ffn_backward(
+            self._ctx, _stream_handle(self.device), _ptr(X), _dtype_code(X), n, X.shape[1], _row_stride(X), _ptr(W_gate), _ptr(W_up),
+            d_ff, _ptr(pre), _ptr(dH), _row_stride(dH), _ptr(dX), X.shape[1], _ptr(dW_gate), _ptr(dW_up)))
+        return dX, dW_gate, dW_up
 
     # ---- profiling ---------------------------------------------------------
     def profile_enable(self, on: bool):

@@ -19,7 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcamera_hip.so")
 BENCH_LIB = os.path.join(HERE, "libcamera_bench.so")
 SOURCES = ["api.hip", "route.hip", "bucket.hip", "gemm.hip", "norm.hip", "rank.hip", "gather.hip", "forward.hip",
-           "compact.hip"]
+           "compact.hip", "logits.hip", "gated.hip"]
 BENCH_SOURCES = ["probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # keep packed-fp32 instruction selection off for every device function

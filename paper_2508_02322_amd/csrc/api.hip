@@ -1078,4 +1078,305 @@ int camera_rank_decisions(camera_ctx* ctx, void* stream_, const float* energy, i
   return run_rank(ctx, stream_, energy, n_micro, seg_offsets, n_seg, r);
 }
 
+// ---- logits ------------------------------------------------------------------------------------------------------
+namespace {
+bool aligned_to(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_logits(camera_ctx* ctx, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature) {
+  if (dtype != CAMERA_F32 && dtype != CAMERA_BF16) return fail(ctx, CAMERA_EDTYPE, "dtype: unknown code %d", dtype);
+  if (n < 0) return fail(ctx, CAMERA_EINVAL, "n: negative");
+  if (vocab < 1 || vocab >= (int64_t(1) << 31) - 1024) return fail(ctx, CAMERA_ESHAPE, "vocab: must be in [1, 2^31 - 1024)");
+  if (n >= int64_t(1) << 31) return fail(ctx, CAMERA_ESHAPE, "n: must be below 2^31");
+  if (ld < vocab) return fail(ctx, CAMERA_ESHAPE, "ld: must be >= vocab");
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
+    return fail(ctx, CAMERA_EINVAL, "temperature: must be positive and finite, its reciprocal too");
+  if (n > 0 && logits == nullptr) return fail(ctx, CAMERA_EINVAL, "logits: NULL");
+  if (!aligned_to(logits, dtype == CAMERA_BF16 ? 2 : 4)) return fail(ctx, CAMERA_ESHAPE, "logits: not aligned to an element");
+  return CAMERA_OK;
+}
+int check_dlogits(camera_ctx* ctx, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, int accumulate,
+                  const void* dlogits, int64_t ldd) {
+  if (n > 0 && dlogits == nullptr) return fail(ctx, CAMERA_EINVAL, "dlogits: NULL");
+  if (ldd < vocab) return fail(ctx, CAMERA_ESHAPE, "ldd: must be >= vocab");
+  if (!aligned_to(dlogits, dtype == CAMERA_BF16 ? 2 : 4)) return fail(ctx, CAMERA_ESHAPE, "dlogits: not aligned to an element");
+  if (dlogits == logits && (accumulate || ldd != ld))
+    return fail(ctx, CAMERA_EINVAL, "dlogits: may be logits only with the same stride and without CAMERA_ACCUMULATE");
+  if (n * (int64_t)camera::logit_grad_parts(dtype, vocab) >= (int64_t(1) << 31))
+    return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
+  return CAMERA_OK;
+}
+int check_teacher(camera_ctx* ctx, int64_t n, const int32_t* idx, const float* logprob, int k) {
+  if (k < 1) return fail(ctx, CAMERA_EINVAL, "k: must be at least 1");
+  if (k > CAMERA_MAX_ALTERNATIVES) return fail(ctx, CAMERA_EUNSUPPORTED, "k: must be at most %d", CAMERA_MAX_ALTERNATIVES);
+  if (n > 0 && (idx == nullptr || logprob == nullptr)) return fail(ctx, CAMERA_EINVAL, "teacher_idx / teacher_logprob: NULL");
+  if (!aligned_to(idx, 4) || !aligned_to(logprob, 4)) return fail(ctx, CAMERA_ESHAPE, "teacher_idx / teacher_logprob: not aligned to an element");
+  return CAMERA_OK;
+}
+float reciprocal(float temperature) { return (float)(1.0 / (double)temperature); }
+}  // namespace
+
+int camera_token_logprobs(camera_ctx* ctx, void* stream_, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld,
+                          float temperature, const int32_t* targets, int top_k, float* logprob, float* entropy, float* stats,
+                          int32_t* top_idx, float* top_logprob) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_logits(ctx, logits, dtype, n, vocab, ld, temperature)) return rc;
+  if (top_k < 0 || top_k > vocab) return fail(ctx, CAMERA_EINVAL, "top_k: must be in [0, vocab]");
+  if (top_k > CAMERA_MAX_ALTERNATIVES) return fail(ctx, CAMERA_EUNSUPPORTED, "top_k: must be at most %d", CAMERA_MAX_ALTERNATIVES);
+  if (n > 0 && (targets == nullptr) != (logprob == nullptr)) return fail(ctx, CAMERA_EINVAL, "targets / logprob: give both or neither");
+  if (n > 0 && top_k > 0 && (top_idx == nullptr || top_logprob == nullptr))
+    return fail(ctx, CAMERA_EINVAL, "top_idx / top_logprob: NULL");
+  if (!aligned_to(targets, 4) || !aligned_to(logprob, 4) || !aligned_to(entropy, 4) || !aligned_to(stats, 4) ||
+      !aligned_to(top_idx, 4) || !aligned_to(top_logprob, 4))
+    return fail(ctx, CAMERA_ESHAPE, "targets / outputs: not aligned to an element");
+  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, false);
+  if (n * plan.parts >= (int64_t(1) << 31)) return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
+  if (n == 0) return CAMERA_OK;
+
+  camera::LogprobArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, top_k, reciprocal(temperature), targets,
+                        logprob, entropy, stats, top_idx, top_logprob, nullptr, nullptr};
+  Carver cv;
+  const size_t most = (size_t)std::max<int64_t>(plan.parts > 1 ? n * plan.parts : 0, camera::kLogitParts);
+  const size_t o_stats = cv.take(most * sizeof(float4)), o_keys = cv.take(most * top_k * sizeof(uint64_t));
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  if (int rc = ensure_workspace(ctx, cv.used)) return rc;
+  a.part_stats = reinterpret_cast<float4*>(static_cast<char*>(ctx->ws) + o_stats);
+  a.part_keys = reinterpret_cast<uint64_t*>(static_cast<char*>(ctx->ws) + o_keys);
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  Bracket b(ctx, stream, CAMERA_K_LOGPROBS);
+  CAMERA_HIP(camera::launch_token_logprobs(stream, dtype, a), "token_logprobs launch");
+  return CAMERA_OK;
+}
+
+int camera_token_logprobs_backward(camera_ctx* ctx, void* stream_, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld,
+                                   float temperature, const int32_t* targets, const float* stats, const float* entropy,
+                                   const float* grad_logprob, const float* grad_entropy, int flags, void* dlogits, int64_t ldd) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_logits(ctx, logits, dtype, n, vocab, ld, temperature)) return rc;
+  if (flags & ~CAMERA_ACCUMULATE) return fail(ctx, CAMERA_EINVAL, "flags: only CAMERA_ACCUMULATE is accepted");
+  if (int rc = check_dlogits(ctx, logits, dtype, n, vocab, ld, flags & CAMERA_ACCUMULATE, dlogits, ldd)) return rc;
+  if (n > 0 && stats == nullptr) return fail(ctx, CAMERA_EINVAL, "stats: NULL");
+  if (n > 0 && grad_logprob == nullptr && grad_entropy == nullptr) return fail(ctx, CAMERA_EINVAL, "grad_logprob / grad_entropy: give one");
+  if (grad_logprob != nullptr && targets == nullptr) return fail(ctx, CAMERA_EINVAL, "targets: NULL with grad_logprob");
+  if (grad_entropy != nullptr && entropy == nullptr) return fail(ctx, CAMERA_EINVAL, "entropy: NULL with grad_entropy");
+  if (!aligned_to(targets, 4) || !aligned_to(stats, 4) || !aligned_to(entropy, 4) || !aligned_to(grad_logprob, 4) || !aligned_to(grad_entropy, 4))
+    return fail(ctx, CAMERA_ESHAPE, "targets / stats / entropy / gradients: not aligned to an element");
+  if (n == 0) return CAMERA_OK;
+
+  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, camera::logit_grad_parts(dtype, vocab), flags & CAMERA_ACCUMULATE,
+                                reciprocal(temperature), stats};
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  Bracket b(ctx, stream, CAMERA_K_LOGPROBS);
+  CAMERA_HIP(camera::launch_token_logprobs_grad(stream, dtype, a, targets, entropy, grad_logprob, grad_entropy),
+             "token_logprobs_backward launch");
+  return CAMERA_OK;
+}
+
+int camera_distill_topk(camera_ctx* ctx, void* stream_, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld,
+                        float temperature, const int32_t* teacher_idx, const float* teacher_logprob, int k, int flags, float* loss,
+                        float* stats) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_logits(ctx, logits, dtype, n, vocab, ld, temperature)) return rc;
+  if (int rc = check_teacher(ctx, n, teacher_idx, teacher_logprob, k)) return rc;
+  if (flags & ~CAMERA_DISTILL_TAIL) return fail(ctx, CAMERA_EINVAL, "flags: only CAMERA_DISTILL_TAIL is accepted");
+  if (n > 0 && (loss == nullptr || stats == nullptr)) return fail(ctx, CAMERA_EINVAL, "loss / stats: NULL");
+  if (!aligned_to(loss, 4) || !aligned_to(stats, 4)) return fail(ctx, CAMERA_ESHAPE, "loss / stats: not aligned to an element");
+  const int tail = flags & CAMERA_DISTILL_TAIL;
+  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, tail != 0);
+  if (n * plan.parts >= (int64_t(1) << 31)) return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
+  if (n == 0) return CAMERA_OK;
+
+  camera::DistillArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, tail, temperature, {teacher_idx, teacher_logprob, k}, loss, stats, nullptr};
+  const size_t most = (size_t)std::max<int64_t>(plan.parts > 1 ? n * plan.parts : 0, camera::kLogitParts);
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  if (int rc = ensure_workspace(ctx, most * sizeof(float4))) return rc;
+  a.part_stats = static_cast<float4*>(ctx->ws);
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  Bracket b(ctx, stream, CAMERA_K_DISTILL);
+  CAMERA_HIP(camera::launch_distill(stream, dtype, a), "distill_topk launch");
+  return CAMERA_OK;
+}
+
+int camera_distill_topk_backward(camera_ctx* ctx, void* stream_, const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld,
+                                 float temperature, const int32_t* teacher_idx, const float* teacher_logprob, int k, const float* stats,
+                                 const float* grad_loss, int flags, void* dlogits, int64_t ldd) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_logits(ctx, logits, dtype, n, vocab, ld, temperature)) return rc;
+  if (int rc = check_teacher(ctx, n, teacher_idx, teacher_logprob, k)) return rc;
+  if (flags & ~(CAMERA_ACCUMULATE | CAMERA_DISTILL_TAIL))
+    return fail(ctx, CAMERA_EINVAL, "flags: only CAMERA_ACCUMULATE and CAMERA_DISTILL_TAIL are accepted");
+  if (int rc = check_dlogits(ctx, logits, dtype, n, vocab, ld, flags & CAMERA_ACCUMULATE, dlogits, ldd)) return rc;
+  if (n > 0 && (stats == nullptr || grad_loss == nullptr)) return fail(ctx, CAMERA_EINVAL, "stats / grad_loss: NULL");
+  if (!aligned_to(stats, 4) || !aligned_to(grad_loss, 4)) return fail(ctx, CAMERA_ESHAPE, "stats / grad_loss: not aligned to an element");
+  if (n == 0) return CAMERA_OK;
+
+  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, camera::logit_grad_parts(dtype, vocab), flags & CAMERA_ACCUMULATE,
+                                reciprocal(temperature), stats};
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  Bracket b(ctx, stream, CAMERA_K_DISTILL);
+  CAMERA_HIP(camera::launch_distill_grad(stream, dtype, a, {teacher_idx, teacher_logprob, k}, flags & CAMERA_DISTILL_TAIL, grad_loss),
+             "distill_topk_backward launch");
+  return CAMERA_OK;
+}
+
+// ---- the gated block ---------------------------------------------------------------------------------------------
+namespace {
+int64_t up_to(int64_t x, int64_t multiple) { return (x + multiple - 1) / multiple * multiple; }
+
+int check_gated(camera_ctx* ctx, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx, const void* W_gate, const void* W_up,
+                int64_t d_ff) {
+  if (int rc = check_common(ctx, X, dtype, n, d_model, ldx)) return rc;
+  if (d_ff < 1 || d_ff > (1 << 24)) return fail(ctx, CAMERA_ESHAPE, "d_ff: must be in [1, 2^24]");
+  if (W_gate == nullptr || W_up == nullptr) return fail(ctx, CAMERA_EINVAL, "W_gate / W_up: NULL");
+  if (!aligned16(W_gate) || !aligned16(W_up)) return fail(ctx, CAMERA_ESHAPE, "W_gate / W_up: not 16-byte aligned");
+  const int tile_m = camera::gemm_tile_m(dtype, d_ff);
+  if (up_to(n, tile_m) / tile_m > 65535 || 2 * up_to(d_ff, tile_m) / tile_m > 65535 || n >= int64_t(1) << 30)
+    return fail(ctx, CAMERA_EUNSUPPORTED, "n / d_ff: too large for one call");
+  return CAMERA_OK;
+}
+// The tables of `groups` groups of `rows` left-operand rows each, all of them in order.
+struct DenseTables {
+  BucketPlan plan;
+  int groups = 0, tile_m = 0, max_tiles = 0;
+  int64_t rows = 0;
+  void take(Carver& cv, int groups_, int64_t rows_, int tile_m_) {
+    groups = groups_;
+    rows = rows_;
+    tile_m = tile_m_;
+    max_tiles = (int)(groups * ((rows + tile_m - 1) / tile_m));
+    plan.take(cv, true, false, groups, groups * rows, max_tiles, 0);
+  }
+};
+// H and / or the projections of every token by the tiled contraction.
+int gated_projections(camera_ctx* ctx, hipStream_t stream, const void* X, int dtype, int64_t d_model, int64_t ldx, const void* W_gate,
+                      const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre, const DenseTables& dense) {
+  const camera::BucketTables t = dense.plan.bind(static_cast<char*>(ctx->ws), ctx->zeros);
+  CAMERA_HIP(camera::launch_dense_tables(stream, dense.rows, dense.groups, dense.tile_m, dense.max_tiles, t), "dense tables launch");
+  camera::GemmEpilogue ep;
+  ep.mode = camera::GemmEpilogue::kGated;
+  ep.hidden = H;
+  ep.ld_hidden = ldh;
+  ep.product = pre;
+  ep.col_gap = (int)up_to(d_ff, 8);
+  ep.ld_product = 2 * ep.col_gap;
+  Bracket b(ctx, stream, CAMERA_K_GEMM);
+  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, X, ldx, d_model, d_ff, 1, W_gate, W_up, 0, dense.max_tiles, t, ep),
+             "gated projections launch");
+  return CAMERA_OK;
+}
+}  // namespace
+
+int camera_gated_ffn(camera_ctx* ctx, void* stream_, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
+                     const void* W_gate, const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_gated(ctx, X, dtype, n, d_model, ldx, W_gate, W_up, d_ff)) return rc;
+  const int v = dtype == CAMERA_BF16 ? 8 : 4;
+  if (n > 0 && H == nullptr && pre == nullptr) return fail(ctx, CAMERA_EINVAL, "H / pre: give one");
+  if (H != nullptr && (ldh < d_ff || ldh % v != 0)) return fail(ctx, CAMERA_ESHAPE, "ldh: must be >= d_ff and a multiple of %d", v);
+  if (!aligned16(H) || !aligned16(pre)) return fail(ctx, CAMERA_ESHAPE, "H / pre: not 16-byte aligned");
+  if (n == 0) return CAMERA_OK;
+
+  Carver cv;
+  DenseTables dense;
+  dense.take(cv, 1, n, camera::gemm_tile_m(dtype, d_ff));
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  if (int rc = ensure_workspace(ctx, cv.used)) return rc;
+  return gated_projections(ctx, static_cast<hipStream_t>(stream_), X, dtype, d_model, ldx, W_gate, W_up, d_ff, H, ldh, pre, dense);
+}
+
+int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
+                              const void* W_gate, const void* W_up, int64_t d_ff, const float* pre, const void* dH, int64_t lddh,
+                              void* dX, int64_t lddx, void* dW_gate, void* dW_up) {
+  if (ctx == nullptr) return fail(nullptr, CAMERA_EINVAL, "ctx: NULL");
+  if (int rc = check_gated(ctx, X, dtype, n, d_model, ldx, W_gate, W_up, d_ff)) return rc;
+  const int v = dtype == CAMERA_BF16 ? 8 : 4;
+  const size_t es = dtype == CAMERA_BF16 ? 2 : 4;
+  if (n > 0 && dH == nullptr) return fail(ctx, CAMERA_EINVAL, "dH: NULL");
+  if (lddh < d_ff) return fail(ctx, CAMERA_ESHAPE, "lddh: must be >= d_ff");
+  if (!aligned_to(dH, es)) return fail(ctx, CAMERA_ESHAPE, "dH: not aligned to an element");
+  if (dX != nullptr && (lddx < d_model || lddx % v != 0))
+    return fail(ctx, CAMERA_ESHAPE, "lddx: must be >= d_model and a multiple of %d", v);
+  if (!aligned16(pre) || !aligned16(dX) || !aligned16(dW_gate) || !aligned16(dW_up))
+    return fail(ctx, CAMERA_ESHAPE, "pre / dX / dW_gate / dW_up: not 16-byte aligned");
+  const bool weights = dW_gate != nullptr || dW_up != nullptr;
+  if (!weights && (dX == nullptr || n == 0)) return CAMERA_OK;
+
+  const int tile_m = camera::gemm_tile_m(dtype, d_ff);
+  const int64_t f_pad = up_to(d_ff, 64), n_pad = up_to(n, 64), half = d_model / 2;
+  const int64_t pre_ld = up_to(d_ff, 8);
+  Carver cv;
+  DenseTables by_token, by_channel;
+  by_token.take(cv, 1, n, tile_m);
+  by_channel.take(cv, 2, d_ff, tile_m);
+  const size_t o_pre = cv.take(pre == nullptr ? sizeof(float) * n * 2 * pre_ld : 0);
+  const size_t o_rows = cv.take(dX != nullptr ? es * n * 2 * f_pad : 0);
+  const size_t o_wt = cv.take(dX != nullptr ? es * d_model * 2 * f_pad : 0);
+  const size_t o_cols = cv.take(weights ? es * 2 * d_ff * n_pad : 0);
+  const size_t o_xt = cv.take(weights ? es * d_model * n_pad : 0);
+  DeviceGuard guard;
+  CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
+  hipStream_t stream = static_cast<hipStream_t>(stream_);
+  if (n == 0) {
+    for (void* w : {dW_gate, dW_up})
+      if (w != nullptr) CAMERA_HIP(camera::launch_zero(stream, w, (int64_t)(es * d_ff * d_model / 16)), "zero launch");
+    return CAMERA_OK;
+  }
+  if (int rc = ensure_workspace(ctx, cv.used)) return rc;
+  char* ws = static_cast<char*>(ctx->ws);
+  if (pre == nullptr) {
+    float* made = reinterpret_cast<float*>(ws + o_pre);
+    if (int rc = gated_projections(ctx, stream, X, dtype, d_model, ldx, W_gate, W_up, d_ff, nullptr, 0, made, by_token)) return rc;
+    pre = made;
+  }
+  {
+    Bracket b(ctx, stream, CAMERA_K_GATED_GRAD);
+    CAMERA_HIP(camera::launch_gated_grad(stream, dtype, pre, pre_ld, dH, lddh, n, d_ff, dX != nullptr ? ws + o_rows : nullptr, f_pad,
+                                         weights ? ws + o_cols : nullptr, n_pad),
+               "gated gradient launch");
+    if (dX != nullptr) {
+      CAMERA_HIP(camera::launch_transpose(stream, dtype, W_gate, d_ff, d_model, d_model, ws + o_wt, 2 * f_pad, f_pad), "transpose launch");
+      CAMERA_HIP(camera::launch_transpose(stream, dtype, W_up, d_ff, d_model, d_model, ws + o_wt + es * f_pad, 2 * f_pad, f_pad),
+                 "transpose launch");
+    }
+    if (weights) CAMERA_HIP(camera::launch_transpose(stream, dtype, X, n, d_model, ldx, ws + o_xt, n_pad, n_pad), "transpose launch");
+  }
+  Bracket b(ctx, stream, CAMERA_K_GEMM);
+  if (dX != nullptr) {  // [dG | dU] times [W_gate; W_up]: the columns of dX in two halves
+    const camera::BucketTables t = by_token.plan.bind(ws, ctx->zeros);
+    CAMERA_HIP(camera::launch_dense_tables(stream, n, 1, tile_m, by_token.max_tiles, t), "dense tables launch");
+    camera::GemmEpilogue ep;
+    ep.mode = camera::GemmEpilogue::kRounded;
+    ep.rounded = dX;
+    ep.ld_product = lddx;
+    ep.col_gap = (int)half;
+    CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, ws + o_rows, 2 * f_pad, 2 * f_pad, half, 1, ws + o_wt,
+                                           ws + o_wt + es * half * 2 * f_pad, 0, by_token.max_tiles, t, ep),
+               "input gradient launch");
+  }
+  if (weights) {  // two groups of left rows, dG^T and dU^T, or one of them
+    const bool both = dW_gate != nullptr && dW_up != nullptr;
+    const int groups = both ? 2 : 1, max_tiles = both ? by_channel.max_tiles : by_channel.max_tiles / 2;
+    const char* left = ws + o_cols + (dW_gate == nullptr ? es * d_ff * n_pad : 0);
+    const camera::BucketTables t = by_channel.plan.bind(ws, ctx->zeros);
+    CAMERA_HIP(camera::launch_dense_tables(stream, d_ff, groups, tile_m, max_tiles, t), "dense tables launch");
+    camera::GemmEpilogue ep;
+    ep.mode = camera::GemmEpilogue::kRounded;
+    ep.rounded = dW_gate != nullptr ? dW_gate : dW_up;
+    ep.ld_product = d_model;
+    ep.col_gap = (int)half;
+    if (both)  // group 1 continues behind group 0's rows: bring it to its own matrix
+      ep.expert_gap = (int64_t)(reinterpret_cast<intptr_t>(dW_up) - reinterpret_cast<intptr_t>(dW_gate)) / (int64_t)es - d_ff * d_model;
+    CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, left, n_pad, n_pad, half, groups, ws + o_xt, ws + o_xt + es * half * n_pad, 0,
+                                           max_tiles, t, ep),
+               "weight gradient launch");
+  }
+  return CAMERA_OK;
+}
+
 }  // extern "C"

@@ -66,8 +66,11 @@ int gemm_tile_m(int dtype, int64_t d_ff);
 //            rounded to bf16 by the bf16 kernel, as float32 by the float32 kernel
 //   kProduct G goes to product[slot][c], U to product[slot][c + col_gap], row stride ld_product; in this mode X is
 //            indexed by bucket slot, not by token (the hidden activations are the left operand)
+//   kGated   silu(G) U goes to hidden[slot][ld_hidden] in the inputs' type (if hidden), G and U to product as above (if product),
+//            X indexed by token; columns d_ff .. the next multiple of 8 (bf16) or 4 are written too, zeros in hidden
+//   kRounded kProduct in the inputs' type: rounded[slot * ld_product + e * expert_gap + c], and c + col_gap
 struct GemmEpilogue {
-  enum Mode { kStats = 0, kHidden = 1, kProduct = 2 };
+  enum Mode { kStats = 0, kHidden = 1, kProduct = 2, kGated = 3, kRounded = 4 };
   int mode = kStats;
   float* part_phi2 = nullptr;
   float* part_max = nullptr;
@@ -83,6 +86,9 @@ struct GemmEpilogue {
   SplitCost split{};
   int64_t part_stride = 0;
   int32_t* parts = nullptr;
+  int64_t ld_hidden = 0;
+  void* rounded = nullptr;
+  int64_t expert_gap = 0;
 };
 hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int64_t ldx, int64_t d_model,
                                int64_t d_ff, int n_experts, const void* W_gate, const void* W_up,
@@ -252,5 +258,71 @@ hipError_t launch_gather_rows(hipStream_t stream, int dtype, const void* W_gate,
 hipError_t launch_gather_cols(hipStream_t stream, int dtype, const void* W_down, int64_t stride_down, int n_experts,
                               int64_t d_ff, int64_t d_model, const int32_t* index, int64_t n_index,
                               int64_t index_base, const int32_t* off, const int32_t* off_ld, void* down_out);
+
+// ---- logits.hip -------------------------------------------------------------
+// Rows of logits are cut into parts of part_len elements (the last one shorter) where there are few of them: parts_of rows x parts
+// workgroups, whose sums (part_stats) and alternatives (part_keys) a second launch joins.
+constexpr int kLogitParts = 2048;     // workgroups that a launch is cut into
+struct LogitPlan {
+  int parts;
+  int64_t part_len;
+};
+// marks: a part's tokens have a bit each in LDS (distillation with the unlisted tokens as a class)
+LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks);
+struct LogprobArgs {
+  const void* logits;
+  int64_t ld, n, vocab, part_len;
+  int parts, top_k;
+  float inv_temperature;
+  const int32_t* targets;
+  float *logprob, *entropy, *stats;
+  int32_t* top_idx;
+  float* top_logprob;
+  float4* part_stats;    // [n][parts]
+  uint64_t* part_keys;   // [n][parts][top_k]
+};
+hipError_t launch_token_logprobs(hipStream_t stream, int dtype, const LogprobArgs& a);
+struct LogitGradArgs {
+  const void* logits;
+  int64_t ld;
+  void* dlogits;         // may be logits, with the same stride
+  int64_t ldd, n, vocab;
+  int parts;             // logit_grad_parts
+  int accumulate;
+  float inv_temperature;
+  const float* stats;
+};
+int logit_grad_parts(int dtype, int64_t vocab);
+hipError_t launch_token_logprobs_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const int32_t* targets,
+                                      const float* entropy, const float* grad_logprob, const float* grad_entropy);
+struct DistillTeacher {
+  const int32_t* idx;    // [n][k]
+  const float* logprob;  // [n][k]
+  int k;
+};
+struct DistillArgs {
+  const void* logits;
+  int64_t ld, n, vocab, part_len;
+  int parts, tail;
+  float temperature;
+  DistillTeacher teacher;
+  float *loss, *stats;
+  float4* part_stats;    // [n][parts]
+};
+hipError_t launch_distill(hipStream_t stream, int dtype, const DistillArgs& a);
+hipError_t launch_distill_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const DistillTeacher& teacher, int tail,
+                               const float* grad_loss);
+
+// ---- gated.hip --------------------------------------------------------------
+// From G, U (pre: float32 [n][2][pre_ld]) and dH: dG = dH U silu'(G) and dU = dH silu(G) in the inputs' type, as rows
+// rows_out [n][2][f_pad] and transposed cols_out [2][d_ff][n_pad], zero in the padding (f_pad, n_pad: multiples of 64).  Either
+// output may be NULL.
+hipError_t launch_gated_grad(hipStream_t stream, int dtype, const float* pre, int64_t pre_ld, const void* dH, int64_t lddh, int64_t n,
+                             int64_t d_ff, void* rows_out, int64_t f_pad, void* cols_out, int64_t n_pad);
+// dst[c][r] = src[r][c] for r < rows, zero for rows <= r < rows_pad (a multiple of 64); cols a multiple of 4.
+hipError_t launch_transpose(hipStream_t stream, int dtype, const void* src, int64_t rows, int64_t cols, int64_t lds, void* dst,
+                            int64_t ldd, int64_t rows_pad);
+// vectors of 16 bytes set to zero
+hipError_t launch_zero(hipStream_t stream, void* dst, int64_t vectors);
 
 }  // namespace camera

@@ -46,6 +46,12 @@ __device__ __forceinline__ float silu_f32(float g) {
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
 }
 
+// Four values rounded to bf16, the first lowest.
+__device__ __forceinline__ uint2 pack_bf16(float a, float b, float c, float d) {
+  auto bits = [](float x) { return (uint32_t)__builtin_bit_cast(uint16_t, __float2bfloat16(x)); };
+  return make_uint2(bits(a) | bits(b) << 16, bits(c) | bits(d) << 16);
+}
+
 // ---------------------------------------------------------------------------
 // bf16 MFMA kernel.
 //   A workgroup is WM x WN waves: 2 x 2 in the built configuration, one wave per SIMD, each with the whole
@@ -96,8 +102,12 @@ constexpr int kChunkM = 4;     // otherwise this many
 //   kEpiListed  : kEpiHidden over the kept micro-experts only: tile channel i of the expert is micro-expert list[i], whose
 //                 weight rows it reads and whose column of the (zeroed) hidden row it writes.  Where the list does not pay it is
 //                 NULL and tile channel i is micro-expert i
-enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3 };
+//   kEpiGated   : silu(gate) * up in the inputs' type -> hidden (if there is one) and gate and up themselves, float32 -> product
+//                 [row][column] and [column + col_gap] (if there is one); columns up to the next multiple of pad_hidden are written too
+//   kEpiRounded : kEpiProduct in the inputs' type -> rounded, the rows of expert e expert_gap elements further on for each e
+enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3, kEpiGated = 4, kEpiRounded = 5 };
 constexpr bool epi_hidden(int epi) { return epi == kEpiHidden || epi == kEpiListed; }
+constexpr bool epi_by_slot(int epi) { return epi == kEpiProduct || epi == kEpiRounded; }  // token rows = bucket slots
 struct EpiArgs {
   float* part_phi2;
   float* part_max;
@@ -115,6 +125,8 @@ struct EpiArgs {
   SplitCost split;         // the kernel chooses the parts by it
   int32_t* parts;          // and leaves their number here; nullptr: k_parts it is
   int64_t blocks;          // workgroups, where not every token tile there may be has one for every part (host)
+  void* rounded;           // kEpiRounded: row stride ld_product
+  int64_t expert_gap;
 };
 
 // One wave instruction of the direct global -> LDS path: lane l's 16 bytes at p (+ IMM) go to LDS bytes
@@ -562,7 +574,7 @@ __device__ __forceinline__ void tile_body16(const TileState<C>& st, int n0, int 
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still be writing LDS at exit
   mfma_drain();                                      // the last MFMAs have written their accumulators
-  if constexpr (C::kAliasAux && EPI != kEpiProduct) __syncthreads();  // the per-tile arrays lie over the ring: every wave has read its last fragments
+  if constexpr (C::kAliasAux && !epi_by_slot(EPI) && EPI != kEpiGated) __syncthreads();  // the per-tile arrays lie over the ring: every wave has read its last fragments
   if constexpr (C::kAliasAux && epi_hidden(EPI)) {
     const_cast<float*>(st.s_a)[threadIdx.x] = a_mine;
     __syncthreads();
@@ -602,6 +614,59 @@ __device__ __forceinline__ void tile_body16(const TileState<C>& st, int n0, int 
     if (col0 < d_ff) {  // output rows and both column halves are multiples of 4 floats: all four lie inside, 16-byte aligned
       if (ep.stream_product) write(std::true_type{});
       else write(std::false_type{});
+    }
+  } else if constexpr (EPI == kEpiRounded) {
+    const int col0 = n0 + st.wave_n * TN * 32 + 4 * lane_col;  // this lane's four columns, of either half
+    if (col0 < d_ff) {
+      __hip_bfloat16* out = static_cast<__hip_bfloat16*>(ep.rounded) + st.expert * ep.expert_gap + col0;
+#pragma unroll
+      for (int i = 0; i < ACT; ++i)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = (WM * i + st.wave_m) * 32 + a * 16 + lane_rows + r;
+            if (row >= st.m_len) continue;
+            __hip_bfloat16* dst = out + (int64_t)(st.row_first + row) * ep.ld_product;
+            *reinterpret_cast<uint2*>(dst) = pack_bf16(acc_g[i][0][a][0][r], acc_g[i][0][a][1][r], acc_g[i][1][a][0][r], acc_g[i][1][a][1][r]);
+            *reinterpret_cast<uint2*>(dst + ep.col_gap) =
+                pack_bf16(acc_u[i][0][a][0][r], acc_u[i][0][a][1][r], acc_u[i][1][a][0][r], acc_u[i][1][a][1][r]);
+          }
+    }
+  } else if constexpr (EPI == kEpiGated) {
+    const int pad_end = (d_ff + ep.pad_hidden - 1) / ep.pad_hidden * ep.pad_hidden;
+    const int col0 = n0 + st.wave_n * TN * 32 + 4 * lane_col;  // this lane's four channels
+    if (col0 < pad_end) {  // rows are multiples of 8 long: all four lie inside
+      uint32_t inside[2] = {0, 0};  // hidden values from d_ff on are zeros
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        if (col0 + s < d_ff) inside[s / 2] |= 0xffffu << (s % 2 * 16);
+#pragma unroll
+      for (int i = 0; i < ACT; ++i)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = (WM * i + st.wave_m) * 32 + a * 16 + lane_rows + r;
+            if (row >= st.m_len) continue;
+            f32x4 g, u;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+              g[s] = acc_g[i][s / 2][a][s % 2][r];
+              u[s] = acc_u[i][s / 2][a][s % 2][r];
+            }
+            if (ep.hidden != nullptr) {
+              uint2 v = pack_bf16(silu_f32(g[0]) * u[0], silu_f32(g[1]) * u[1], silu_f32(g[2]) * u[2], silu_f32(g[3]) * u[3]);
+              v.x &= inside[0];
+              v.y &= inside[1];
+              *reinterpret_cast<uint2*>(static_cast<__hip_bfloat16*>(ep.hidden) + (int64_t)(st.row_first + row) * ep.ld_hidden + col0) = v;
+            }
+            if (ep.product != nullptr) {
+              float* dst = ep.product + (int64_t)(st.row_first + row) * ep.ld_product + col0;
+              *reinterpret_cast<f32x4*>(dst) = g;
+              *reinterpret_cast<f32x4*>(dst + ep.col_gap) = u;
+            }
+          }
     }
   } else if constexpr (EPI == kEpiListed) {
     const int col0 = n0 + st.wave_n * TN * 32 + 4 * lane_col;  // this lane's four entries
@@ -762,7 +827,7 @@ __device__ __forceinline__ void run_tile(const TileWork& w, const __hip_bfloat16
   // their Lambda is exactly 0 (finite projections times a = 0), so no load in the K loop is conditional.
   for (int r = tid; r < BM; r += C::kThreads) {
     const int rr = r < m_len ? r : 0;
-    if constexpr (EPI == kEpiProduct) s_tok[r] = row_first + rr;  // A rows are the bucket slots themselves
+    if constexpr (epi_by_slot(EPI)) s_tok[r] = row_first + rr;  // A rows are the bucket slots themselves
     else s_tok[r] = perm ? perm[row_first + rr] : w.tok_first + rr;
     s_a[r] = r < m_len ? (w_perm ? w_perm[row_first + rr] : 1.0f) : 0.0f;
   }
@@ -1273,7 +1338,7 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
     const int row = lrow + 32 * p;
     const int rr = row_first + (row < m_len ? row : 0);
     int64_t tok;
-    if constexpr (EPI == kEpiProduct) tok = rr;  // the left operand is indexed by bucket slot
+    if constexpr (epi_by_slot(EPI)) tok = rr;  // the left operand is indexed by bucket slot
     else tok = perm ? perm[rr] : rr - offsets[e];
     x_src[p] = X + tok * ldx + lk;
   }
@@ -1341,6 +1406,22 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
         if (row < m_len && c < d_ff) {
           ep.product[out_row * ep.ld_product + c] = acc_g[b][i];
           ep.product[out_row * ep.ld_product + c + ep.col_gap] = acc_u[b][i];
+        }
+      } else if constexpr (EPI == kEpiRounded) {
+        if (row < m_len && c < d_ff) {
+          float* dst = static_cast<float*>(ep.rounded) + e * ep.expert_gap + out_row * ep.ld_product + c;
+          dst[0] = acc_g[b][i];
+          dst[ep.col_gap] = acc_u[b][i];
+        }
+      } else if constexpr (EPI == kEpiGated) {
+        const int pad_end = (d_ff + ep.pad_hidden - 1) / ep.pad_hidden * ep.pad_hidden;
+        if (row < m_len && c < pad_end) {
+          if (ep.hidden != nullptr)
+            static_cast<float*>(ep.hidden)[out_row * ep.ld_hidden + c] = c < d_ff ? silu_f32(acc_g[b][i]) * acc_u[b][i] : 0.0f;
+          if (ep.product != nullptr) {
+            ep.product[out_row * ep.ld_product + c] = acc_g[b][i];
+            ep.product[out_row * ep.ld_product + c + ep.col_gap] = acc_u[b][i];
+          }
         }
       } else {
         const float lam = s_a[row] * silu_f32(acc_g[b][i]) * acc_u[b][i];
@@ -1479,7 +1560,7 @@ static hipError_t launch_bf16(hipStream_t stream, const void* X, int64_t ldx, in
   auto kern = tail ? grouped_gemm_bf16_kernel<C, true, EPI> : grouped_gemm_bf16_kernel<C, false, EPI>;
   static OncePerDevice lds_allowed[2];
   if (hipError_t err = allow_lds(lds_allowed[tail], reinterpret_cast<const void*>(kern), C::kSmemBytes); err != hipSuccess) return err;
-  if (EPI != kEpiStats && d_ff % 4 != 0) return hipErrorInvalidValue;  // the epilogues that write rows write four channels at a time
+  if (EPI != kEpiStats && EPI != kEpiGated && d_ff % 4 != 0) return hipErrorInvalidValue;  // the epilogues that write rows write four channels at a time
   const int64_t n_tiles_n = (d_ff + C::BN - 1) / C::BN;
   int64_t n_blocks = (max_tiles * n_tiles_n + kXcds - 1) / kXcds * kXcds;
   if (ep.blocks != 0) n_blocks = ep.blocks;
@@ -1496,7 +1577,11 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
                                int64_t stride_gu, int max_tiles, const BucketTables& t, const GemmEpilogue& e) {
   if (max_tiles <= 0) return hipSuccess;
   EpiArgs ep{e.part_phi2, e.part_max, e.hidden, e.keep, nullptr, e.product, e.ld_product, e.col_gap, d_ff, 0, e.stream_product ? 1 : 0,
-             e.split_plan.most_parts, e.part_stride, e.split, e.parts, e.split_plan.blocks};
+             e.split_plan.most_parts, e.part_stride, e.split, e.parts, e.split_plan.blocks, e.rounded, e.expert_gap};
+  if (e.mode == GemmEpilogue::kGated) {
+    ep.ld_hidden = e.ld_hidden;
+    ep.pad_hidden = dtype == CAMERA_BF16 ? 8 : 4;
+  }
   if (ep.k_parts < 1 || ep.k_parts > kMostParts) return hipErrorInvalidValue;
   if (dtype == CAMERA_BF16) {
     switch (e.mode) {
@@ -1506,6 +1591,10 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
         return launch_bf16<kEpiHidden>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kProduct:
         return launch_bf16<kEpiProduct>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
+      case GemmEpilogue::kGated:
+        return launch_bf16<kEpiGated>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
+      case GemmEpilogue::kRounded:
+        return launch_bf16<kEpiRounded>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       default:
         return hipErrorInvalidValue;
     }
@@ -1514,8 +1603,10 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
   if (n_blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   auto kern = e.mode == GemmEpilogue::kStats    ? grouped_gemm_f32_kernel<kEpiStats>
               : e.mode == GemmEpilogue::kHidden ? grouped_gemm_f32_kernel<kEpiHidden>
+              : e.mode == GemmEpilogue::kGated  ? grouped_gemm_f32_kernel<kEpiGated>
+              : e.mode == GemmEpilogue::kRounded ? grouped_gemm_f32_kernel<kEpiRounded>
                                                 : grouped_gemm_f32_kernel<kEpiProduct>;
-  if (e.mode < GemmEpilogue::kStats || e.mode > GemmEpilogue::kProduct) return hipErrorInvalidValue;
+  if (e.mode < GemmEpilogue::kStats || e.mode > GemmEpilogue::kRounded) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kern, launch_grid(n_blocks), dim3(256), 0, stream, static_cast<const float*>(X), ldx, (int)d_model,
                      (int)d_ff, static_cast<const float*>(W_gate), static_cast<const float*>(W_up), stride_gu, t.offsets,
                      t.tile_offset, t.tile_expert, t.perm, t.w_perm, n_experts, ep);

@@ -1,0 +1,774 @@
+// What a model answers with, row by row of its logits Z [n x vocab]: the log probabilities of given tokens with the entropy and
+// the most likely alternatives, the distance from a teacher whose most likely tokens are known, and the gradients of both.
+//
+// With p = softmax(z / T), m = max z and S = sum exp((z - m) / T):
+//   log p_v = (z_v - m) / T - log S,      H = -sum p log p = log S - (1 / S) sum exp(d_v) d_v,  d_v = (z_v - m) / T
+// One pass over a row keeps, per thread, the largest logit so far, the sum of exponentials relative to it and the sum weighted
+// by the exponents, all in float32, and rescales the sums when the largest logit grows.  d_v is taken as a difference first, so
+// that logits of any size (the type's lowest value as a mask among them) stay exact; a logit of -inf adds nothing.
+//
+// All of it is bound by reading the logits once (and writing the gradient once).
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "camera_internal.h"
+
+namespace camera {
+namespace {
+
+constexpr int kThreads = 512;  // >= CAMERA_MAX_ALTERNATIVES: the k-th largest of the threads' maxima exists
+constexpr int kWaves = kThreads / kWave;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.693147180559945309417f;
+constexpr float kFloor = -1.0e4f;  // exponents are clamped here: exp2 of it is 0, and 0 times it is 0
+static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "one thread for every alternative");
+
+// 16 bytes of a row.  Rows start where the caller's do, at any element: the loads and stores carry the element's alignment only.
+template <class T>
+struct Pack;
+template <>
+struct Pack<float> {
+  static constexpr int N = 4;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void get(Raw r, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t bits = r[i];  // (a bit cast of the vector's element itself takes its first one, with this compiler)
+      v[i] = __builtin_bit_cast(float, bits);
+    }
+  }
+  static __device__ __forceinline__ Raw put(const float* v) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, v[i]);
+    return r;
+  }
+  static __device__ __forceinline__ float one(float x) { return x; }
+  static __device__ __forceinline__ float round(float x) { return x; }
+};
+template <>
+struct Pack<__bf16> {
+  static constexpr int N = 8;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ void get(Raw r, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, r[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, r[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ Raw put(const float* v) {
+    typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, Pair{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
+    return r;
+  }
+  static __device__ __forceinline__ float one(__bf16 x) { return (float)x; }
+  static __device__ __forceinline__ __bf16 round(float x) { return (__bf16)x; }
+};
+
+// ---- reductions over the workgroup ---------------------------------------------------------------------------------
+template <class X, class F>
+__device__ __forceinline__ X wave_all(X x, F f) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) x = f(x, __shfl_xor(x, d));
+  return x;
+}
+// Every thread gets the result, taken in the same order; slots: kWaves values of LDS.  Barriers inside.
+template <class X, class F>
+__device__ __forceinline__ X block_all(X x, F f, X* slots) {
+  x = wave_all(x, f);
+  __syncthreads();  // the slots' earlier use is over
+  if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = x;
+  __syncthreads();
+  X all = slots[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) all = f(all, slots[w]);
+  return all;
+}
+struct Add {
+  template <class X>
+  __device__ __forceinline__ X operator()(X a, X b) const { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+
+// ---- the running sums ----------------------------------------------------------------------------------------------
+// scale = log2(e) / T.  s = sum exp2((z - m) scale), t = sum exp2(d) d with d in powers of two.
+struct Running {
+  float m = -INFINITY, s = 0.0f, t = 0.0f;
+};
+// What an empty row or thread is taken relative to.
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
+// The sums relative to the larger maximum `m`.
+__device__ __forceinline__ void rescale(Running& r, float m, float scale) {
+  const float d = fmaxf((r.m - reference(m)) * scale, kFloor), c = __builtin_amdgcn_exp2f(d);
+  r.t = c * fmaf(r.s, d, r.t);
+  r.s *= c;
+  r.m = m;
+}
+template <bool ENTROPY, int N>
+__device__ __forceinline__ void add_values(Running& r, const float* z, float scale) {
+  float m = r.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, z[i]);
+  rescale(r, m, scale);
+  const float ref = reference(m);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = fmaxf((z[i] - ref) * scale, kFloor), e = __builtin_amdgcn_exp2f(d);
+    r.s += e;
+    if constexpr (ENTROPY) r.t = fmaf(e, d, r.t);
+  }
+}
+struct Slots {
+  float f[2][kWaves];
+  double d[kWaves];
+};
+__device__ __forceinline__ Running block_running(Running r, float scale, Slots& slots) {
+  rescale(r, block_all(r.m, Max{}, slots.f[0]), scale);
+  r.s = block_all(r.s, Add{}, slots.f[1]);
+  r.t = block_all(r.t, Add{}, slots.f[0]);
+  return r;
+}
+
+// ---- one part of a row ---------------------------------------------------------------------------------------------
+// Thread j's stripe is the vectors j, j + kThreads, ... of the part, and element j of what is left behind the whole vectors.
+template <class T>
+struct RowPart {
+  static constexpr int N = Pack<T>::N;
+  using Raw = typename Pack<T>::Raw;
+  const T* z;  // first element of the part
+  int first;   // its index in the row
+  int vecs, rest;
+  __device__ RowPart(const T* row, int64_t first_, int len) : z(row + first_), first((int)first_), vecs(len / N), rest(len % N) {}
+  __device__ __forceinline__ Raw load(int v) const { return *reinterpret_cast<const Raw*>(z + (int64_t)v * N); }
+  __device__ __forceinline__ float left(int i) const { return Pack<T>::one(z[(int64_t)vecs * N + i]); }
+};
+
+// Marks of a part's listed elements, a bit each.
+constexpr int kMaxListed = 1 << 18;  // elements of a part with marks: 32 KiB of LDS, five workgroups a compute unit
+
+template <class T, bool ENTROPY, bool LISTED>
+__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks) {
+  constexpr int N = Pack<T>::N, U = 4;  // vectors in flight per thread
+  Running r;
+  auto one = [&](typename Pack<T>::Raw raw, int v, float* z) {
+    Pack<T>::get(raw, z);
+    if constexpr (LISTED) {
+      const unsigned bits = N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u;
+      if (bits != 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = bits >> i & 1 ? -INFINITY : z[i];
+      }
+    }
+  };
+  int v = threadIdx.x;
+  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads) {
+    typename Pack<T>::Raw raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = p.load(v + u * kThreads);
+    float z[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
+    add_values<ENTROPY, U * N>(r, z, scale);
+  }
+  for (; v < p.vecs; v += kThreads) {
+    float z[N];
+    one(p.load(v), v, z);
+    add_values<ENTROPY, N>(r, z, scale);
+  }
+  if ((int)threadIdx.x < p.rest) {
+    float z = p.left(threadIdx.x);
+    if constexpr (LISTED) {
+      const int at = p.vecs * N + threadIdx.x;
+      if (marks[at >> 3] >> (at & 7) & 1) z = -INFINITY;
+    }
+    add_values<ENTROPY, 1>(r, &z, scale);
+  }
+  return r;
+}
+
+// ---- the largest k -------------------------------------------------------------------------------------------------
+// A token's key orders as (logit, lower index first) does: the logit's bits made monotone, then the index turned round.  -0 and
+// +0 are equal.  0 stands for no token: -inf (and NaN) are never alternatives.
+__device__ __forceinline__ uint32_t order_bits(float z) {
+  if (!(z > -INFINITY)) return 0;
+  const uint32_t b = __builtin_bit_cast(uint32_t, z + 0.0f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float of_order_bits(uint32_t o) {
+  return __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint64_t make_key(uint32_t bits, int index) { return (uint64_t)bits << 32 | (0xffffffffu - (uint32_t)index); }
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
+
+constexpr int kCandidates = 2048;  // >= the elements of a part that has fewer stripes than alternatives are wanted
+struct SelectSmem {
+  uint32_t largest[kThreads];
+  int32_t stripes[kThreads];
+  uint64_t keys[kCandidates];
+  int32_t hist[256];
+  uint32_t tau;
+  int32_t n_stripes, n_keys;
+  uint64_t prefix;
+  int32_t want;
+};
+
+// Where keys come from: stripe j has positions() places of up to N keys.
+template <class T>
+struct LogitKeys {
+  const RowPart<T>& p;
+  __device__ __forceinline__ int positions() const { return (p.vecs + kThreads - 1) / kThreads + (p.rest != 0 ? 1 : 0); }
+  template <class F>
+  __device__ __forceinline__ void at(int stripe, int pos, F&& f) const {
+    constexpr int N = Pack<T>::N;
+    const int whole = (p.vecs + kThreads - 1) / kThreads;
+    if (pos < whole) {
+      const int v = pos * kThreads + stripe;
+      if (v < p.vecs) {
+        float z[N];
+        Pack<T>::get(p.load(v), z);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(order_bits(z[i]), p.first + v * N + i);
+      }
+    } else if (stripe < p.rest) {
+      f(order_bits(p.left(stripe)), p.first + p.vecs * N + stripe);
+    }
+  }
+};
+struct ListKeys {
+  const uint64_t* keys;
+  int n;
+  __device__ __forceinline__ int positions() const { return (n + kThreads - 1) / kThreads; }
+  template <class F>
+  __device__ __forceinline__ void at(int stripe, int pos, F&& f) const {
+    const int i = pos * kThreads + stripe;
+    if (i < n) {
+      const uint64_t key = keys[i];
+      f((uint32_t)(key >> 32), key_index(key));
+    }
+  }
+};
+
+// out(r, key) for the k largest keys of a source in falling order, key 0 where there are fewer.  `largest`: order bits of the
+// largest value of the thread's stripe.  At least k stripes have a value as large as the k-th largest of the stripes' maxima, so that
+// is a lower bound of the k-th largest value; the values not below it lie in the stripes whose maximum is not, mostly k of them, which
+// are read again (they come from the caches).  A candidate's place is the number of larger keys, so the order in which candidates
+// are found does not show.  Where more values reach the bound than there is room for (ties: a constant row, a mask by the type's
+// lowest value), the k-th largest key is found by its digits, eight passes over the source.
+template <class SOURCE, class OUT>
+__device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem& sm, OUT&& out) {
+  const int tid = threadIdx.x;
+  sm.largest[tid] = largest;
+  if (tid == 0) {
+    sm.tau = 0;
+    sm.n_stripes = 0;
+    sm.n_keys = 0;
+  }
+  __syncthreads();
+  int before = 0;
+  for (int j = 0; j < kThreads; j += 4) {
+    const uint4 o = *reinterpret_cast<const uint4*>(&sm.largest[j]);
+    before += (o.x > largest || (o.x == largest && j < tid)) + (o.y > largest || (o.y == largest && j + 1 < tid)) +
+              (o.z > largest || (o.z == largest && j + 2 < tid)) + (o.w > largest || (o.w == largest && j + 3 < tid));
+  }
+  if (before == k - 1) sm.tau = largest;  // the places are different: one thread
+  __syncthreads();
+  const uint32_t tau = sm.tau;
+  if (largest >= tau && largest != 0) sm.stripes[atomicAdd(&sm.n_stripes, 1)] = tid;
+  __syncthreads();
+  const int n_stripes = sm.n_stripes, positions = src.positions();
+  auto collect = [&](uint64_t floor_key) {
+    for (int w = tid; w < n_stripes * positions; w += kThreads)
+      src.at(sm.stripes[w % n_stripes], w / n_stripes, [&](uint32_t bits, int index) {
+        if (bits < tau || bits == 0) return;
+        const uint64_t key = make_key(bits, index);
+        if (key < floor_key) return;
+        const int at = atomicAdd(&sm.n_keys, 1);
+        if (at < kCandidates) sm.keys[at] = key;
+      });
+  };
+  collect(0);
+  __syncthreads();
+  int n_keys = sm.n_keys;
+  if (n_keys > kCandidates) {
+    uint64_t prefix = 0;
+    int want = k;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+      __syncthreads();
+      if (tid < 256) sm.hist[tid] = 0;
+      __syncthreads();
+      for (int pos = 0; pos < positions; ++pos)
+        src.at(tid, pos, [&](uint32_t bits, int index) {
+          if (bits < tau || bits == 0) return;
+          const uint64_t key = make_key(bits, index);
+          if (shift < 56 && (key ^ prefix) >> (shift + 8) != 0) return;
+          // lanes that count the same digit as the first one add once
+          const int digit = (int)(key >> shift & 255), lead = __builtin_amdgcn_readfirstlane(digit);
+          const uint64_t same = __ballot(digit == lead);
+          if (digit != lead) atomicAdd(&sm.hist[digit], 1);
+          else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
+        });
+      __syncthreads();
+      if (tid == 0) {
+        int digit = 255;
+        for (; digit > 0 && want > sm.hist[digit]; --digit) want -= sm.hist[digit];
+        sm.prefix = prefix | (uint64_t)digit << shift;
+        sm.want = want;
+      }
+      __syncthreads();
+      prefix = sm.prefix;
+      want = sm.want;
+    }
+    if (tid == 0) sm.n_keys = 0;
+    __syncthreads();
+    collect(prefix);
+    __syncthreads();
+    n_keys = sm.n_keys;  // k
+  }
+  for (int i = tid; i < n_keys; i += kThreads) {
+    const uint64_t key = sm.keys[i];
+    int place = 0;
+#pragma unroll 4
+    for (int j = 0; j < n_keys; ++j) place += sm.keys[j] > key;
+    if (place < k) out(place, key);
+  }
+  for (int r = n_keys + tid; r < k; r += kThreads) out(r, (uint64_t)0);
+}
+
+// ---- log probabilities, entropy, alternatives ----------------------------------------------------------------------
+template <class T>
+__device__ __forceinline__ void finish_logprobs(const Running& r, const LogprobArgs& a, int64_t row) {
+  const bool none = r.m == -INFINITY;
+  const float log_sum = none ? 0.0f : logf(r.s);
+  if (threadIdx.x == 0) {
+    if (a.stats) {
+      a.stats[2 * row] = r.m;
+      a.stats[2 * row + 1] = log_sum;
+    }
+    if (a.entropy) a.entropy[row] = none ? 0.0f : log_sum - r.t / r.s * kLn2;
+    if (a.logprob) {
+      const int64_t target = a.targets[row];
+      float lp = 0.0f;
+      if (target >= 0 && target < a.vocab)
+        lp = none ? -INFINITY
+                  : (Pack<T>::one(static_cast<const T*>(a.logits)[row * a.ld + target]) - r.m) * a.inv_temperature - log_sum;
+      a.logprob[row] = lp;
+    }
+  }
+}
+__device__ __forceinline__ void write_alternative(const LogprobArgs& a, const Running& r, float log_sum, int64_t row, int place,
+                                                  uint64_t key) {
+  const bool none = key == 0;
+  a.top_idx[row * a.top_k + place] = none ? -1 : key_index(key);
+  a.top_logprob[row * a.top_k + place] =
+      none ? -INFINITY : (of_order_bits((uint32_t)(key >> 32)) - r.m) * a.inv_temperature - log_sum;
+}
+
+// A workgroup has a part of a row; with one part a row it ends it, else it leaves its sums and its alternatives' keys.
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(LogprobArgs a) {
+  __shared__ Slots slots;
+  const int64_t block = linear_block();
+  const int64_t row = block / a.parts;
+  if (row >= a.n) return;
+  const int part = (int)(block - row * a.parts);
+  const int64_t first = part * a.part_len;
+  const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, (int)min(a.part_len, a.vocab - first));
+  const float scale = a.inv_temperature * kLog2e;
+  Running mine = stream_part<T, true, false>(p, scale, nullptr);
+  const uint32_t largest = order_bits(mine.m);
+  const Running r = block_running(mine, scale, slots);
+  if (a.parts == 1) finish_logprobs<T>(r, a, row);
+  else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
+  if constexpr (TOP) {
+    __shared__ SelectSmem sm;
+    const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
+    select_top(LogitKeys<T>{p}, largest, a.top_k, sm, [&](int place, uint64_t key) {
+      if (a.parts == 1) write_alternative(a, r, log_sum, row, place, key);
+      else a.part_keys[block * a.top_k + place] = key;
+    });
+  }
+}
+
+// A row's parts put together, in their order.
+__device__ __forceinline__ Running join_parts(const float4* part_stats, int parts, float scale, Slots& slots) {
+  Running mine;
+  for (int i = threadIdx.x; i < parts; i += kThreads) {
+    const float4 s = part_stats[i];
+    Running other;
+    other.m = s.x;
+    other.s = s.y;
+    other.t = s.z;
+    const float m = fmaxf(mine.m, other.m);
+    rescale(mine, m, scale);
+    rescale(other, m, scale);
+    mine.s += other.s;
+    mine.t += other.t;
+  }
+  return block_running(mine, scale, slots);
+}
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) {
+  __shared__ Slots slots;
+  const int64_t row = linear_block();
+  if (row >= a.n) return;
+  const float scale = a.inv_temperature * kLog2e;
+  const Running r = join_parts(a.part_stats + row * a.parts, a.parts, scale, slots);
+  finish_logprobs<T>(r, a, row);
+  if constexpr (TOP) {
+    __shared__ SelectSmem sm;
+    const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
+    const ListKeys keys{a.part_keys + row * a.parts * a.top_k, a.parts * a.top_k};
+    uint32_t largest = 0;
+    for (int pos = 0; pos < keys.positions(); ++pos) keys.at(threadIdx.x, pos, [&](uint32_t bits, int) { largest = max(largest, bits); });
+    select_top(keys, largest, a.top_k, sm, [&](int place, uint64_t key) { write_alternative(a, r, log_sum, row, place, key); });
+  }
+}
+
+// ---- gradients -----------------------------------------------------------------------------------------------------
+// A workgroup has kGradVecs vectors of a row; every thread has its vectors' loads in flight together.
+constexpr int kGradUnroll = 4;
+template <class T>
+struct GradPart {
+  static constexpr int N = Pack<T>::N, kLen = kThreads * kGradUnroll * N;
+  using Raw = typename Pack<T>::Raw;
+  const T* z;
+  T* out;
+  int64_t first;  // of the part, in the row
+  int len;
+  bool accumulate;
+
+  // out (+)= f(z, index in the part) over the part; f gets a vector's values and leaves the gradient in their place.
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    const int vecs = len / N, rest = len - vecs * N, tid = threadIdx.x;
+    Raw raw[kGradUnroll], old[kGradUnroll];
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) {
+      const int v = tid + u * kThreads;
+      if (v < vecs) {
+        raw[u] = *reinterpret_cast<const Raw*>(z + v * N);
+        if (accumulate) old[u] = *reinterpret_cast<const Raw*>(out + v * N);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) {
+      const int v = tid + u * kThreads;
+      if (v < vecs) {
+        float x[N];
+        Pack<T>::get(raw[u], x);
+        f(x, v * N, std::integral_constant<int, N>{});
+        if (accumulate) {
+          float y[N];
+          Pack<T>::get(old[u], y);
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] += y[i];
+        }
+        *reinterpret_cast<Raw*>(out + v * N) = Pack<T>::put(x);
+      }
+    }
+    if (tid < rest) {
+      const int at = vecs * N + tid;
+      float x = Pack<T>::one(z[at]);
+      f(&x, at, std::integral_constant<int, 1>{});
+      if (accumulate) x += Pack<T>::one(out[at]);
+      out[at] = Pack<T>::round(x);
+    }
+  }
+  __device__ __forceinline__ void zero() const {
+    const int vecs = len / N, rest = len - vecs * N;
+    for (int v = threadIdx.x; v < vecs; v += kThreads) *reinterpret_cast<Raw*>(out + v * N) = Raw{0, 0, 0, 0};
+    if ((int)threadIdx.x < rest) out[vecs * N + threadIdx.x] = Pack<T>::round(0.0f);
+  }
+};
+template <class T>
+__device__ __forceinline__ GradPart<T> grad_part(const LogitGradArgs& a, int64_t row, int part) {
+  GradPart<T> p;
+  p.first = (int64_t)part * GradPart<T>::kLen;
+  p.len = (int)min((int64_t)GradPart<T>::kLen, a.vocab - p.first);
+  p.z = static_cast<const T*>(a.logits) + row * a.ld + p.first;
+  p.out = static_cast<T*>(a.dlogits) + row * a.ldd + p.first;
+  p.accumulate = a.accumulate != 0;
+  return p;
+}
+
+// d logprob[t] / dz_v = (1[v = t] - p_v) / T,  d H / dz_v = -p_v (log p_v + H) / T
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a, const int32_t* __restrict__ targets,
+                                                                 const float* __restrict__ entropy,
+                                                                 const float* __restrict__ grad_logprob,
+                                                                 const float* __restrict__ grad_entropy) {
+  const int64_t block = linear_block();
+  const int64_t row = block / a.parts;
+  if (row >= a.n) return;
+  const GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  const int64_t target = targets ? (int64_t)targets[row] : -1;
+  const float m = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
+  const float one = grad_logprob && target >= 0 && target < a.vocab ? grad_logprob[row] * a.inv_temperature : 0.0f;
+  const float two = grad_entropy ? grad_entropy[row] * a.inv_temperature : 0.0f;
+  if ((one == 0.0f && two == 0.0f) || m == -INFINITY) {  // the gradient is 0 whatever the logits are
+    if (!p.accumulate) p.zero();
+    return;
+  }
+  const float inv_t = a.inv_temperature, h = two != 0.0f ? entropy[row] : 0.0f;
+  const int64_t at = target - p.first;  // in this part, or not
+  p.each([&](float* x, int v, auto count) {
+    constexpr int N = decltype(count)::value;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float lp = fmaxf((x[i] - m) * inv_t - log_sum, kFloor);
+      x[i] = __builtin_amdgcn_exp2f(lp * kLog2e) * -fmaf(two, lp + h, one);
+    }
+    if (one != 0.0f && at >= v && at < v + N) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (at == v + i) x[i] += one;
+    }
+  });
+}
+
+// ---- distillation --------------------------------------------------------------------------------------------------
+// The teacher's distribution q over the tokens it lists, and with `tail` the rest of its probability as one class of all tokens it
+// does not list; the student's p over the same classes.  Kullback-Leibler divergence:
+//   loss = sum_j q_j (log q_j - log p_j)  [+ q_r (log q_r - log p_r)],  q_r = 1 - sum q_j,  p_r = sum of p_v over the unlisted v
+// p_r is summed over the unlisted tokens themselves (1 - sum p_j would cancel): a bit per token of the part marks the listed ones.
+// The few values of the listed tokens are handled in float64.
+
+// Entry `j` of the row's teacher list (thread j < k): whether it counts (it names a token, has a probability and is the first to
+// name it).  Barriers inside; ids: k ints of LDS.
+__device__ __forceinline__ bool entry_counts(const DistillTeacher& t, int64_t row, int64_t vocab, int32_t* ids, int* id, float* value) {
+  const int j = threadIdx.x;
+  *id = -1;
+  *value = -INFINITY;
+  if (j < t.k) {
+    *id = t.idx[row * t.k + j];
+    *value = t.logprob[row * t.k + j];
+    ids[j] = *id;
+  }
+  __syncthreads();
+  bool ok = j < t.k && *id >= 0 && *id < vocab && *value > -INFINITY;
+  if (ok)
+    for (int i = 0; i < j; ++i) ok = ok && ids[i] != *id;
+  return ok;
+}
+
+template <class T>
+__device__ __forceinline__ void finish_distill(const Running& rest, const DistillArgs& a, int64_t row, int id, float value, bool ok,
+                                               Slots& slots) {
+  // rest: the sums over all tokens, or with tail over the unlisted ones
+  const double inv_t = 1.0 / (double)a.temperature;
+  const float z = ok ? Pack<T>::one(static_cast<const T*>(a.logits)[row * a.ld + id]) : -INFINITY;
+  float m = rest.m;
+  double sum = rest.s;
+  if (a.tail) {
+    m = fmaxf(m, block_all(z, Max{}, slots.f[0]));
+    const double ref = reference(m);
+    sum = block_all(z > -INFINITY ? exp(((double)z - ref) * inv_t) : 0.0, Add{}, slots.d);
+    if (rest.m > -INFINITY) sum += (double)rest.s * exp(((double)rest.m - ref) * inv_t);
+  }
+  const double log_sum = m == -INFINITY ? 0.0 : log(sum);
+  double norm = 0.0, log_q = value;
+  if (!a.tail) {
+    const float tm = block_all(ok ? value : -INFINITY, Max{}, slots.f[0]);
+    const double ref = reference(tm);
+    const double total = block_all(ok ? exp(((double)value - ref) * inv_t) : 0.0, Add{}, slots.d);
+    norm = total > 0.0 ? ref * inv_t + log(total) : 0.0;
+    log_q = (double)value * inv_t - norm;
+  }
+  const double q = ok ? exp(log_q) : 0.0;
+  const double log_p = z > -INFINITY ? ((double)z - (double)m) * inv_t - log_sum : -INFINITY;
+  double loss = block_all(q > 0.0 ? q * (log_q - log_p) : 0.0, Add{}, slots.d);
+  double mass = block_all(q, Add{}, slots.d), log_ratio = -INFINITY;
+  if (a.tail && rest.m > -INFINITY) {
+    const double left = fmax(0.0, 1.0 - mass);
+    const double log_rest = ((double)rest.m - (double)m) * inv_t + log((double)rest.s) - log_sum;
+    mass += left;
+    if (left > 0.0) {
+      log_ratio = log(left) - log_rest;
+      loss += left * log_ratio;
+    }
+  }
+  if (threadIdx.x == 0) {
+    a.loss[row] = (float)loss;
+    float* st = a.stats + row * CAMERA_DISTILL_STATS;
+    st[0] = m;
+    st[1] = (float)log_sum;
+    st[2] = (float)norm;
+    st[3] = (float)mass;
+    st[4] = (float)log_ratio;
+  }
+}
+
+template <class T, bool TAIL>
+__global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
+  __shared__ Slots slots;
+  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  const int64_t block = linear_block();
+  const int64_t row = block / a.parts;
+  if (row >= a.n) return;
+  const int part = (int)(block - row * a.parts);
+  const int64_t first = part * a.part_len;
+  const int len = (int)min(a.part_len, a.vocab - first);
+  const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
+  const float scale = kLog2e / a.temperature;
+  int id = -1;
+  float value = -INFINITY;
+  bool ok = false;
+  if (TAIL || a.parts == 1) ok = entry_counts(a.teacher, row, a.vocab, ids, &id, &value);
+  Running mine;
+  if constexpr (TAIL) {
+    __shared__ __align__(16) uint32_t marks[kMaxListed / 32];
+    for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
+    __syncthreads();
+    if (ok && id >= first && id < first + len) atomicOr(&marks[(id - first) >> 5], 1u << ((id - first) & 31));
+    __syncthreads();
+    mine = stream_part<T, false, true>(p, scale, reinterpret_cast<const unsigned char*>(marks));
+  } else {
+    mine = stream_part<T, false, false>(p, scale, nullptr);
+  }
+  const Running r = block_running(mine, scale, slots);
+  if (a.parts == 1) finish_distill<T>(r, a, row, id, value, ok, slots);
+  else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, 0.0f, 0.0f);
+}
+template <class T>
+__global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
+  __shared__ Slots slots;
+  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  const int64_t row = linear_block();
+  if (row >= a.n) return;
+  int id;
+  float value;
+  const bool ok = entry_counts(a.teacher, row, a.vocab, ids, &id, &value);
+  const Running r = join_parts(a.part_stats + row * a.parts, a.parts, kLog2e / a.temperature, slots);
+  finish_distill<T>(r, a, row, id, value, ok, slots);
+}
+
+// d loss / dz_v = (mass p_v - q_v) / T for a listed v, p_v (mass - q_r / p_r) / T for an unlisted one (mass alone without tail):
+// the second for every token of the part, then the first over the listed ones.  A listed token's logit and old gradient
+// are read before anything is written (dlogits may be logits), and its value is written after the workgroup's stores are done.
+template <class T>
+__global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a, DistillTeacher teacher, int tail,
+                                                                const float* __restrict__ grad_loss) {
+  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  const int64_t block = linear_block();
+  const int64_t row = block / a.parts;
+  if (row >= a.n) return;
+  const GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  const float* st = a.stats + row * CAMERA_DISTILL_STATS;
+  const float m = st[0], log_sum = st[1], norm = st[2], mass = st[3], log_ratio = st[4];
+  const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
+  if (g == 0.0f || m == -INFINITY) {  // the gradient is 0 whatever the logits are
+    if (!p.accumulate) p.zero();
+    return;
+  }
+  int id;
+  float value;
+  const bool ok = entry_counts(teacher, row, a.vocab, ids, &id, &value);
+  const int64_t at = (int64_t)id - p.first;
+  const bool here = ok && at >= 0 && at < p.len;
+  float listed = 0.0f;
+  if (here) {
+    const float lp = fmaxf((Pack<T>::one(p.z[at]) - m) * inv_t - log_sum, kFloor);
+    const float lq = tail ? value : value * inv_t - norm;
+    listed = g * (mass * expf(lp) - expf(lq));
+    if (p.accumulate) listed += Pack<T>::one(p.out[at]);
+  }
+  __syncthreads();  // the reads above are done before the part is written
+  // p_v (mass - q_r / p_r) as one exponential: the ratio may be as large as p_r is small, and mass is then nothing beside it
+  const float scale2 = inv_t * kLog2e, factor = mass - expf(log_ratio), c = factor < 0.0f ? -g : g;
+  const float log2_factor = factor == 0.0f ? kFloor : (log_ratio > 80.0f ? log_ratio : logf(fabsf(factor))) * kLog2e - log_sum * kLog2e;
+  p.each([&](float* x, int, auto count) {
+    constexpr int N = decltype(count)::value;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = c * __builtin_amdgcn_exp2f(fmaf(x[i] - m, scale2, log2_factor));
+  });
+  __syncthreads();  // and written before the listed tokens are
+  if (here) p.out[at] = Pack<T>::round(listed);
+}
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+}  // namespace
+
+// Parts of a row: as many as give the chip kLogitParts workgroups, each with at least a vector for every thread.
+LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks) {
+  const int64_t vec = dtype == CAMERA_BF16 ? 8 : 4, least = kThreads * vec;
+  int64_t parts = std::max<int64_t>(1, kLogitParts / std::max<int64_t>(1, n));
+  parts = std::min(parts, std::max<int64_t>(1, vocab / least));
+  if (marks) parts = std::max(parts, (vocab + kMaxListed - 1) / kMaxListed);
+  parts = std::max(parts, (vocab + (int64_t(1) << 30) - 1) >> 30);  // a part's elements are counted in 31 bits
+  LogitPlan plan;
+  plan.part_len = round_up((vocab + parts - 1) / parts, least / 8);
+  plan.parts = (int)((vocab + plan.part_len - 1) / plan.part_len);
+  return plan;
+}
+
+#define CAMERA_BY_TYPE(dtype, CALL)    \
+  do {                                 \
+    if ((dtype) == CAMERA_BF16) {      \
+      using T = __bf16;                \
+      CALL;                            \
+    } else {                           \
+      using T = float;                 \
+      CALL;                            \
+    }                                  \
+  } while (0)
+
+hipError_t launch_token_logprobs(hipStream_t stream, int dtype, const LogprobArgs& a) {
+  const int64_t blocks = a.n * a.parts;
+  if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  const dim3 block(kThreads);
+  CAMERA_BY_TYPE(dtype, {
+    if (a.top_k > 0) hipLaunchKernelGGL((logprobs_kernel<T, true>), launch_grid(blocks), block, 0, stream, a);
+    else hipLaunchKernelGGL((logprobs_kernel<T, false>), launch_grid(blocks), block, 0, stream, a);
+    if (a.parts > 1) {
+      if (a.top_k > 0) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), launch_grid(a.n), block, 0, stream, a);
+      else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), launch_grid(a.n), block, 0, stream, a);
+    }
+  });
+  return hipGetLastError();
+}
+
+int logit_grad_parts(int dtype, int64_t vocab) {
+  const int64_t len = dtype == CAMERA_BF16 ? GradPart<__bf16>::kLen : GradPart<float>::kLen;
+  return (int)((vocab + len - 1) / len);
+}
+
+hipError_t launch_token_logprobs_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const int32_t* targets,
+                                      const float* entropy, const float* grad_logprob, const float* grad_entropy) {
+  const int64_t blocks = a.n * a.parts;
+  if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  CAMERA_BY_TYPE(dtype, hipLaunchKernelGGL((logprobs_grad_kernel<T>), launch_grid(blocks), dim3(kThreads), 0, stream, a, targets,
+                                           entropy, grad_logprob, grad_entropy));
+  return hipGetLastError();
+}
+
+hipError_t launch_distill(hipStream_t stream, int dtype, const DistillArgs& a) {
+  const int64_t blocks = a.n * a.parts;
+  if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  if (a.tail && a.part_len > kMaxListed) return hipErrorInvalidValue;
+  const dim3 block(kThreads);
+  CAMERA_BY_TYPE(dtype, {
+    if (a.tail) hipLaunchKernelGGL((distill_kernel<T, true>), launch_grid(blocks), block, 0, stream, a);
+    else hipLaunchKernelGGL((distill_kernel<T, false>), launch_grid(blocks), block, 0, stream, a);
+    if (a.parts > 1) hipLaunchKernelGGL((distill_join_kernel<T>), launch_grid(a.n), block, 0, stream, a);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_distill_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const DistillTeacher& teacher, int tail,
+                               const float* grad_loss) {
+  const int64_t blocks = a.n * a.parts;
+  if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  CAMERA_BY_TYPE(dtype, hipLaunchKernelGGL((distill_grad_kernel<T>), launch_grid(blocks), dim3(kThreads), 0, stream, a, teacher, tail,
+                                           grad_loss));
+  return hipGetLastError();
+}
+
+}  // namespace camera
