@@ -111,11 +111,13 @@ __device__ __forceinline__ void rescale(Running& r, float m, float scale) {
   r.s *= c;
   r.m = m;
 }
+// Adds N values; returns the largest of them.
 template <bool ENTROPY, int N>
-__device__ __forceinline__ void add_values(Running& r, const float* z, float scale) {
-  float m = r.m;
+__device__ __forceinline__ float add_values(Running& r, const float* z, float scale) {
+  float largest = z[0];
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, z[i]);
+  for (int i = 1; i < N; ++i) largest = fmaxf(largest, z[i]);
+  const float m = fmaxf(r.m, largest);
   rescale(r, m, scale);
   const float ref = reference(m);
 #pragma unroll
@@ -124,6 +126,7 @@ __device__ __forceinline__ void add_values(Running& r, const float* z, float sca
     r.s += e;
     if constexpr (ENTROPY) r.t = fmaf(e, d, r.t);
   }
+  return largest;
 }
 struct Slots {
   float f[2][kWaves];
@@ -136,64 +139,7 @@ __device__ __forceinline__ Running block_running(Running r, float scale, Slots& 
   return r;
 }
 
-// ---- one part of a row ---------------------------------------------------------------------------------------------
-// Thread j's stripe is the vectors j, j + kThreads, ... of the part, and element j of what is left behind the whole vectors.
-template <class T>
-struct RowPart {
-  static constexpr int N = Pack<T>::N;
-  using Raw = typename Pack<T>::Raw;
-  const T* z;  // first element of the part
-  int first;   // its index in the row
-  int vecs, rest;
-  __device__ RowPart(const T* row, int64_t first_, int len) : z(row + first_), first((int)first_), vecs(len / N), rest(len % N) {}
-  __device__ __forceinline__ Raw load(int v) const { return *reinterpret_cast<const Raw*>(z + (int64_t)v * N); }
-  __device__ __forceinline__ float left(int i) const { return Pack<T>::one(z[(int64_t)vecs * N + i]); }
-};
-
-// Marks of a part's listed elements, a bit each.
-constexpr int kMaxListed = 1 << 18;  // elements of a part with marks: 32 KiB of LDS, five workgroups a compute unit
-
-template <class T, bool ENTROPY, bool LISTED>
-__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks) {
-  constexpr int N = Pack<T>::N, U = 4;  // vectors in flight per thread
-  Running r;
-  auto one = [&](typename Pack<T>::Raw raw, int v, float* z) {
-    Pack<T>::get(raw, z);
-    if constexpr (LISTED) {
-      const unsigned bits = N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u;
-      if (bits != 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = bits >> i & 1 ? -INFINITY : z[i];
-      }
-    }
-  };
-  int v = threadIdx.x;
-  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads) {
-    typename Pack<T>::Raw raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = p.load(v + u * kThreads);
-    float z[U * N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
-    add_values<ENTROPY, U * N>(r, z, scale);
-  }
-  for (; v < p.vecs; v += kThreads) {
-    float z[N];
-    one(p.load(v), v, z);
-    add_values<ENTROPY, N>(r, z, scale);
-  }
-  if ((int)threadIdx.x < p.rest) {
-    float z = p.left(threadIdx.x);
-    if constexpr (LISTED) {
-      const int at = p.vecs * N + threadIdx.x;
-      if (marks[at >> 3] >> (at & 7) & 1) z = -INFINITY;
-    }
-    add_values<ENTROPY, 1>(r, &z, scale);
-  }
-  return r;
-}
-
-// ---- the largest k -------------------------------------------------------------------------------------------------
+// ---- a token's place in the order ---------------------------------------------------------------------------------
 // A token's key orders as (logit, lower index first) does: the logit's bits made monotone, then the index turned round.  -0 and
 // +0 are equal.  0 stands for no token: -inf (and NaN) are never alternatives.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -207,36 +153,124 @@ __device__ __forceinline__ float of_order_bits(uint32_t o) {
 __device__ __forceinline__ uint64_t make_key(uint32_t bits, int index) { return (uint64_t)bits << 32 | (0xffffffffu - (uint32_t)index); }
 __device__ __forceinline__ int key_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 
+// ---- one part of a row ---------------------------------------------------------------------------------------------
+// Thread j's stripe is the vectors j, j + kThreads, ... of the part, and element j of what is left behind the whole vectors.  A
+// stripe is cut into cells of per_cell groups of kUnroll vectors (what is left belongs to the last one).
+constexpr int kUnroll = 4;  // vectors in flight per thread
+constexpr int kCells = 16;
+template <class T>
+struct RowPart {
+  static constexpr int N = Pack<T>::N;
+  using Raw = typename Pack<T>::Raw;
+  const T* z;  // first element of the part
+  int first;   // its index in the row
+  int vecs, rest;
+  int per_cell, cells;
+  __device__ RowPart(const T* row, int64_t first_, int len) : z(row + first_), first((int)first_), vecs(len / N), rest(len % N) {
+    const int groups = (vecs + kUnroll * kThreads - 1) / (kUnroll * kThreads);
+    per_cell = groups / kCells + 1;
+    cells = groups / per_cell + 1;  // <= kCells
+  }
+  __device__ __forceinline__ Raw load(int v) const { return *reinterpret_cast<const Raw*>(z + (int64_t)v * N); }
+  __device__ __forceinline__ float left(int i) const { return Pack<T>::one(z[(int64_t)vecs * N + i]); }
+};
+
+// Marks of a part's listed elements, a bit each.
+constexpr int kMaxListed = 1 << 18;  // elements of a part with marks: 32 KiB of LDS, four workgroups a compute unit
+
+// The thread's sums over its stripe.  cell_max (CELLS): upper half of the order bits of every cell's largest value, [cell][thread].
+template <class T, bool ENTROPY, bool LISTED, bool CELLS>
+__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks, uint16_t* cell_max) {
+  constexpr int N = Pack<T>::N, U = kUnroll;
+  const int tid = threadIdx.x;
+  Running r;
+  auto one = [&](typename Pack<T>::Raw raw, int v, float* z) {
+    Pack<T>::get(raw, z);
+    if constexpr (LISTED) {
+      const unsigned bits = N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u;
+      if (bits != 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = bits >> i & 1 ? -INFINITY : z[i];
+      }
+    }
+  };
+  float largest = -INFINITY;  // of the cell
+  int cell = 0, groups = 0;
+  int v = tid;
+  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads) {
+    typename Pack<T>::Raw raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = p.load(v + u * kThreads);
+    float z[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
+    const float top = add_values<ENTROPY, U * N>(r, z, scale);
+    if constexpr (CELLS) {
+      largest = fmaxf(largest, top);
+      if (++groups == p.per_cell) {
+        cell_max[cell++ * kThreads + tid] = (uint16_t)(order_bits(largest) >> 16);
+        largest = -INFINITY;
+        groups = 0;
+      }
+    }
+  }
+  for (; v < p.vecs; v += kThreads) {
+    float z[N];
+    one(p.load(v), v, z);
+    largest = fmaxf(largest, add_values<ENTROPY, N>(r, z, scale));
+  }
+  if constexpr (CELLS) {
+    for (; cell < p.cells; ++cell) {
+      if (cell == p.cells - 1 && tid < p.rest) largest = fmaxf(largest, p.left(tid));
+      cell_max[cell * kThreads + tid] = (uint16_t)(order_bits(largest) >> 16);
+      largest = -INFINITY;
+    }
+  }
+  if (tid < p.rest) {
+    float z = p.left(tid);
+    if constexpr (LISTED) {
+      const int at = p.vecs * N + tid;
+      if (marks[at >> 3] >> (at & 7) & 1) z = -INFINITY;
+    }
+    add_values<ENTROPY, 1>(r, &z, scale);
+  }
+  return r;
+}
+
+// ---- the largest k -------------------------------------------------------------------------------------------------
 constexpr int kCandidates = 2048;  // >= the elements of a part that has fewer stripes than alternatives are wanted
+constexpr int kChosen = 1024;
 struct SelectSmem {
   uint32_t largest[kThreads];
-  int32_t stripes[kThreads];
+  uint16_t cell_max[kCells * kThreads];  // of the rows' cells
+  int32_t chosen[kChosen];               // cells that may hold candidates: cell * kThreads + stripe
   uint64_t keys[kCandidates];
   int32_t hist[256];
-  uint32_t tau;
-  int32_t n_stripes, n_keys;
+  uint32_t bound;
+  int32_t n_chosen, n_keys;
   uint64_t prefix;
   int32_t want;
 };
 
-// Where keys come from: stripe j has positions() places of up to N keys.
+// Where keys come from: every stripe has cells() cells of positions() places of up to N keys.
 template <class T>
 struct LogitKeys {
   const RowPart<T>& p;
-  __device__ __forceinline__ int positions() const { return (p.vecs + kThreads - 1) / kThreads + (p.rest != 0 ? 1 : 0); }
+  __device__ __forceinline__ int cells() const { return p.cells; }
+  __device__ __forceinline__ int positions() const { return p.per_cell * kUnroll + (p.rest != 0 ? 1 : 0); }
   template <class F>
-  __device__ __forceinline__ void at(int stripe, int pos, F&& f) const {
+  __device__ __forceinline__ void at(int stripe, int cell, int pos, F&& f) const {
     constexpr int N = Pack<T>::N;
-    const int whole = (p.vecs + kThreads - 1) / kThreads;
+    const int whole = p.per_cell * kUnroll;
     if (pos < whole) {
-      const int v = pos * kThreads + stripe;
+      const int v = (cell * whole + pos) * kThreads + stripe;
       if (v < p.vecs) {
         float z[N];
         Pack<T>::get(p.load(v), z);
 #pragma unroll
         for (int i = 0; i < N; ++i) f(order_bits(z[i]), p.first + v * N + i);
       }
-    } else if (stripe < p.rest) {
+    } else if (cell == p.cells - 1 && stripe < p.rest) {
       f(order_bits(p.left(stripe)), p.first + p.vecs * N + stripe);
     }
   }
@@ -244,9 +278,10 @@ struct LogitKeys {
 struct ListKeys {
   const uint64_t* keys;
   int n;
+  __device__ __forceinline__ int cells() const { return 1; }
   __device__ __forceinline__ int positions() const { return (n + kThreads - 1) / kThreads; }
   template <class F>
-  __device__ __forceinline__ void at(int stripe, int pos, F&& f) const {
+  __device__ __forceinline__ void at(int stripe, int, int pos, F&& f) const {
     const int i = pos * kThreads + stripe;
     if (i < n) {
       const uint64_t key = keys[i];
@@ -256,64 +291,83 @@ struct ListKeys {
 };
 
 // out(r, key) for the k largest keys of a source in falling order, key 0 where there are fewer.  `largest`: order bits of the
-// largest value of the thread's stripe.  At least k stripes have a value as large as the k-th largest of the stripes' maxima, so that
-// is a lower bound of the k-th largest value; the values not below it lie in the stripes whose maximum is not, mostly k of them, which
-// are read again (they come from the caches).  A candidate's place is the number of larger keys, so the order in which candidates
-// are found does not show.  Where more values reach the bound than there is room for (ties: a constant row, a mask by the type's
-// lowest value), the k-th largest key is found by its digits, eight passes over the source.
+// largest value of the thread's stripe; sm.cell_max: their upper half for its cells.  At least k stripes have a value as large as
+// the k-th largest of the stripes' maxima, so that is a lower bound of the k-th largest value.  One wave finds it, bit by bit, with
+// its lower 16 bits left 0 (all that a bf16 value has; counting for every maximum how many are larger took the workgroup 7 us).
+// The values not below it lie in the cells whose maximum is not, mostly k of them, which are read again, from the caches.  A
+// candidate's place is the number of larger keys, so the order in which candidates are found does not show.  Where more values
+// reach the bound than there is room for (ties: a constant row, a mask by the type's lowest value), the k-th largest key is
+// found by its digits, eight passes over the source.
 template <class SOURCE, class OUT>
 __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem& sm, OUT&& out) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, cells = src.cells(), positions = src.positions();
   sm.largest[tid] = largest;
   if (tid == 0) {
-    sm.tau = 0;
-    sm.n_stripes = 0;
+    sm.n_chosen = 0;
     sm.n_keys = 0;
   }
   __syncthreads();
-  int before = 0;
-  for (int j = 0; j < kThreads; j += 4) {
-    const uint4 o = *reinterpret_cast<const uint4*>(&sm.largest[j]);
-    before += (o.x > largest || (o.x == largest && j < tid)) + (o.y > largest || (o.y == largest && j + 1 < tid)) +
-              (o.z > largest || (o.z == largest && j + 2 < tid)) + (o.w > largest || (o.w == largest && j + 3 < tid));
+  if (tid < kWave) {
+    uint32_t mine[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mine[w] = sm.largest[w * kWave + tid];
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t higher = bound | 1u << bit;
+      int reached = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) reached += (int)__popcll(__ballot(mine[w] >= higher));
+      if (reached >= k) bound = higher;
+    }
+    if (tid == 0) sm.bound = bound;
   }
-  if (before == k - 1) sm.tau = largest;  // the places are different: one thread
   __syncthreads();
-  const uint32_t tau = sm.tau;
-  if (largest >= tau && largest != 0) sm.stripes[atomicAdd(&sm.n_stripes, 1)] = tid;
+  const uint32_t bound = sm.bound;
+  for (int c = 0; c < cells; ++c) {
+    const uint32_t m = sm.cell_max[c * kThreads + tid];
+    if (m >= bound >> 16 && m != 0) {
+      const int at = atomicAdd(&sm.n_chosen, 1);
+      if (at < kChosen) sm.chosen[at] = c * kThreads + tid;
+    }
+  }
   __syncthreads();
-  const int n_stripes = sm.n_stripes, positions = src.positions();
-  auto collect = [&](uint64_t floor_key) {
-    for (int w = tid; w < n_stripes * positions; w += kThreads)
-      src.at(sm.stripes[w % n_stripes], w / n_stripes, [&](uint32_t bits, int index) {
-        if (bits < tau || bits == 0) return;
-        const uint64_t key = make_key(bits, index);
-        if (key < floor_key) return;
-        const int at = atomicAdd(&sm.n_keys, 1);
-        if (at < kCandidates) sm.keys[at] = key;
-      });
+  const int n_chosen = sm.n_chosen;
+  auto add_key = [&](uint64_t key) {
+    const int at = atomicAdd(&sm.n_keys, 1);
+    if (at < kCandidates) sm.keys[at] = key;
   };
-  collect(0);
-  __syncthreads();
+  if (n_chosen <= kChosen) {
+    for (int w = tid; w < n_chosen * positions; w += kThreads) {
+      const int c = sm.chosen[w % n_chosen];
+      src.at(c % kThreads, c / kThreads, w / n_chosen, [&](uint32_t bits, int index) {
+        if (bits >= bound && bits != 0) add_key(make_key(bits, index));
+      });
+    }
+    __syncthreads();
+  }
   int n_keys = sm.n_keys;
-  if (n_keys > kCandidates) {
+  if (n_chosen > kChosen || n_keys > kCandidates) {
+    auto every = [&](auto&& f) {
+      for (int c = 0; c < cells; ++c)
+        for (int pos = 0; pos < positions; ++pos)
+          src.at(tid, c, pos, [&](uint32_t bits, int index) {
+            if (bits >= bound && bits != 0) f(make_key(bits, index));
+          });
+    };
     uint64_t prefix = 0;
     int want = k;
     for (int shift = 56; shift >= 0; shift -= 8) {
       __syncthreads();
       if (tid < 256) sm.hist[tid] = 0;
       __syncthreads();
-      for (int pos = 0; pos < positions; ++pos)
-        src.at(tid, pos, [&](uint32_t bits, int index) {
-          if (bits < tau || bits == 0) return;
-          const uint64_t key = make_key(bits, index);
-          if (shift < 56 && (key ^ prefix) >> (shift + 8) != 0) return;
-          // lanes that count the same digit as the first one add once
-          const int digit = (int)(key >> shift & 255), lead = __builtin_amdgcn_readfirstlane(digit);
-          const uint64_t same = __ballot(digit == lead);
-          if (digit != lead) atomicAdd(&sm.hist[digit], 1);
-          else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
-        });
+      every([&](uint64_t key) {
+        if (shift < 56 && (key ^ prefix) >> (shift + 8) != 0) return;
+        // lanes that count the same digit as the first one add once
+        const int digit = (int)(key >> shift & 255), lead = __builtin_amdgcn_readfirstlane(digit);
+        const uint64_t same = __ballot(digit == lead);
+        if (digit != lead) atomicAdd(&sm.hist[digit], 1);
+        else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
+      });
       __syncthreads();
       if (tid == 0) {
         int digit = 255;
@@ -327,9 +381,11 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
     }
     if (tid == 0) sm.n_keys = 0;
     __syncthreads();
-    collect(prefix);
+    every([&](uint64_t key) {
+      if (key >= prefix) add_key(key);
+    });
     __syncthreads();
-    n_keys = sm.n_keys;  // k
+    n_keys = sm.n_keys;  // k, or as many as there are
   }
   for (int i = tid; i < n_keys; i += kThreads) {
     const uint64_t key = sm.keys[i];
@@ -381,15 +437,18 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(LogprobArgs a) {
   const int64_t first = part * a.part_len;
   const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, (int)min(a.part_len, a.vocab - first));
   const float scale = a.inv_temperature * kLog2e;
-  Running mine = stream_part<T, true, false>(p, scale, nullptr);
-  const uint32_t largest = order_bits(mine.m);
+  SelectSmem* select = nullptr;
+  if constexpr (TOP) {
+    __shared__ SelectSmem sm;
+    select = &sm;
+  }
+  const Running mine = stream_part<T, true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr);
   const Running r = block_running(mine, scale, slots);
   if (a.parts == 1) finish_logprobs<T>(r, a, row);
   else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
   if constexpr (TOP) {
-    __shared__ SelectSmem sm;
     const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
-    select_top(LogitKeys<T>{p}, largest, a.top_k, sm, [&](int place, uint64_t key) {
+    select_top(LogitKeys<T>{p}, order_bits(mine.m), a.top_k, *select, [&](int place, uint64_t key) {
       if (a.parts == 1) write_alternative(a, r, log_sum, row, place, key);
       else a.part_keys[block * a.top_k + place] = key;
     });
@@ -426,7 +485,8 @@ __global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) 
     const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
     const ListKeys keys{a.part_keys + row * a.parts * a.top_k, a.parts * a.top_k};
     uint32_t largest = 0;
-    for (int pos = 0; pos < keys.positions(); ++pos) keys.at(threadIdx.x, pos, [&](uint32_t bits, int) { largest = max(largest, bits); });
+    for (int pos = 0; pos < keys.positions(); ++pos) keys.at(threadIdx.x, 0, pos, [&](uint32_t bits, int) { largest = max(largest, bits); });
+    sm.cell_max[threadIdx.x] = (uint16_t)(largest >> 16);
     select_top(keys, largest, a.top_k, sm, [&](int place, uint64_t key) { write_alternative(a, r, log_sum, row, place, key); });
   }
 }
@@ -628,9 +688,9 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
     __syncthreads();
     if (ok && id >= first && id < first + len) atomicOr(&marks[(id - first) >> 5], 1u << ((id - first) & 31));
     __syncthreads();
-    mine = stream_part<T, false, true>(p, scale, reinterpret_cast<const unsigned char*>(marks));
+    mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr);
   } else {
-    mine = stream_part<T, false, false>(p, scale, nullptr);
+    mine = stream_part<T, false, false, false>(p, scale, nullptr, nullptr);
   }
   const Running r = block_running(mine, scale, slots);
   if (a.parts == 1) finish_distill<T>(r, a, row, id, value, ok, slots);
