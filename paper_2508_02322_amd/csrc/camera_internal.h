@@ -262,7 +262,7 @@ hipError_t launch_gather_cols(hipStream_t stream, int dtype, const void* W_down,
 // ---- logits.hip -------------------------------------------------------------
 // Rows of logits are cut into parts of part_len elements (the last one shorter) where there are few of them: parts_of rows x parts
 // workgroups, whose sums (part_stats) and alternatives (part_keys) a second launch joins.
-constexpr int kLogitParts = 2048;     // workgroups that a launch is cut into
+constexpr int kLogitParts = 1024;     // workgroups that a launch is cut into: as many as the chip holds at once
 struct LogitPlan {
   int parts;
   int64_t part_len;

@@ -130,7 +130,6 @@ __device__ __forceinline__ float add_values(Running& r, const float* z, float sc
 }
 struct Slots {
   float f[2][kWaves];
-  double d[kWaves];
 };
 __device__ __forceinline__ Running block_running(Running r, float scale, Slots& slots) {
   rescale(r, block_all(r.m, Max{}, slots.f[0]), scale);
@@ -204,9 +203,8 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
     float z[U * N];
 #pragma unroll
     for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
-    const float top = add_values<ENTROPY, U * N>(r, z, scale);
+    largest = fmaxf(largest, add_values<ENTROPY, U * N>(r, z, scale));
     if constexpr (CELLS) {
-      largest = fmaxf(largest, top);
       if (++groups == p.per_cell) {
         cell_max[cell++ * kThreads + tid] = (uint16_t)(order_bits(largest) >> 16);
         largest = -INFINITY;
@@ -214,11 +212,18 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
       }
     }
   }
-  for (; v < p.vecs; v += kThreads) {
-    float z[N];
-    one(p.load(v), v, z);
-    largest = fmaxf(largest, add_values<ENTROPY, N>(r, z, scale));
-  }
+  // up to three vectors more, their loads in flight together: one by one they took a latency each
+  typename Pack<T>::Raw raw[U - 1];
+#pragma unroll
+  for (int u = 0; u < U - 1; ++u)
+    if (v + u * kThreads < p.vecs) raw[u] = p.load(v + u * kThreads);
+#pragma unroll
+  for (int u = 0; u < U - 1; ++u)
+    if (v + u * kThreads < p.vecs) {
+      float z[N];
+      one(raw[u], v + u * kThreads, z);
+      largest = fmaxf(largest, add_values<ENTROPY, N>(r, z, scale));
+    }
   if constexpr (CELLS) {
     for (; cell < p.cells; ++cell) {
       if (cell == p.cells - 1 && tid < p.rest) largest = fmaxf(largest, p.left(tid));
@@ -240,6 +245,8 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
 // ---- the largest k -------------------------------------------------------------------------------------------------
 constexpr int kCandidates = 2048;  // >= the elements of a part that has fewer stripes than alternatives are wanted
 constexpr int kChosen = 1024;
+// Up to this many candidates are placed by counting the larger ones (their square, over the workgroup's lanes), more by sorting.
+constexpr int kCounted = 128;
 struct SelectSmem {
   uint32_t largest[kThreads];
   uint16_t cell_max[kCells * kThreads];  // of the rows' cells
@@ -294,8 +301,8 @@ struct ListKeys {
 // largest value of the thread's stripe; sm.cell_max: their upper half for its cells.  At least k stripes have a value as large as
 // the k-th largest of the stripes' maxima, so that is a lower bound of the k-th largest value.  One wave finds it, bit by bit, with
 // its lower 16 bits left 0 (all that a bf16 value has; counting for every maximum how many are larger took the workgroup 7 us).
-// The values not below it lie in the cells whose maximum is not, mostly k of them, which are read again, from the caches.  A
-// candidate's place is the number of larger keys, so the order in which candidates are found does not show.  Where more values
+// The values not below it lie in the cells whose maximum is not, mostly k of them, which are read again, from the caches.  The
+// keys are all different, so the order in which candidates are found does not show.  Where more values
 // reach the bound than there is room for (ties: a constant row, a mask by the type's lowest value), the k-th largest key is
 // found by its digits, eight passes over the source.
 template <class SOURCE, class OUT>
@@ -387,12 +394,29 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
     __syncthreads();
     n_keys = sm.n_keys;  // k, or as many as there are
   }
-  for (int i = tid; i < n_keys; i += kThreads) {
-    const uint64_t key = sm.keys[i];
-    int place = 0;
+  if (n_keys <= kCounted) {
+    if (tid < n_keys) {
+      const uint64_t key = sm.keys[tid];
+      int place = 0;
 #pragma unroll 4
-    for (int j = 0; j < n_keys; ++j) place += sm.keys[j] > key;
-    if (place < k) out(place, key);
+      for (int j = 0; j < n_keys; ++j) place += sm.keys[j] > key;
+      if (place < k) out(place, key);
+    }
+  } else {
+    int size = 2 * kCounted;
+    while (size < n_keys) size *= 2;
+    for (int i = n_keys + tid; i < size; i += kThreads) sm.keys[i] = 0;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+      for (int apart = run / 2; apart > 0; apart /= 2) {
+        for (int c = tid; c < size / 2; c += kThreads) {
+          const int i = 2 * c - (c & (apart - 1)), j = i + apart;  // the pairs `apart` from each other
+          const uint64_t x = sm.keys[i], y = sm.keys[j];
+          if ((x < y) == ((i & run) == 0)) sm.keys[i] = y, sm.keys[j] = x;
+        }
+        __syncthreads();
+      }
+    for (int r = tid; r < min(k, n_keys); r += kThreads) out(r, sm.keys[r]);
   }
   for (int r = n_keys + tid; r < k; r += kThreads) out(r, (uint64_t)0);
 }
@@ -600,51 +624,80 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a
 // p_r is summed over the unlisted tokens themselves (1 - sum p_j would cancel): a bit per token of the part marks the listed ones.
 // The few values of the listed tokens are handled in float64.
 
-// Entry `j` of the row's teacher list (thread j < k): whether it counts (it names a token, has a probability and is the first to
-// name it).  Barriers inside; ids: k ints of LDS.
-__device__ __forceinline__ bool entry_counts(const DistillTeacher& t, int64_t row, int64_t vocab, int32_t* ids, int* id, float* value) {
-  const int j = threadIdx.x;
-  *id = -1;
-  *value = -INFINITY;
-  if (j < t.k) {
-    *id = t.idx[row * t.k + j];
-    *value = t.logprob[row * t.k + j];
-    ids[j] = *id;
+// A row's teacher list in LDS.  An entry counts if it names a token, has a probability and is the first to name its token.
+struct TeacherSmem {
+  int32_t id[CAMERA_MAX_ALTERNATIVES];
+  float value[CAMERA_MAX_ALTERNATIVES];
+};
+__device__ __forceinline__ void load_teacher(const DistillTeacher& t, int64_t row, TeacherSmem& sm) {
+  for (int j = threadIdx.x; j < t.k; j += kThreads) {
+    sm.id[j] = t.idx[row * t.k + j];
+    sm.value[j] = t.logprob[row * t.k + j];
   }
   __syncthreads();
-  bool ok = j < t.k && *id >= 0 && *id < vocab && *value > -INFINITY;
+}
+__device__ __forceinline__ bool entry_counts(const TeacherSmem& sm, int j, int64_t vocab) {
+  const int id = sm.id[j];
+  bool ok = id >= 0 && id < vocab && sm.value[j] > -INFINITY;
   if (ok)
-    for (int i = 0; i < j; ++i) ok = ok && ids[i] != *id;
+    for (int i = 0; i < j; ++i) ok = ok && sm.id[i] != id;
   return ok;
 }
 
+// rest: the sums over all tokens, or with tail over the unlisted ones.  One wave does it, lane l the entries l, l + 64, ...: in
+// float64 the exponentials and logarithms of eight waves took as long as the row's own.
 template <class T>
-__device__ __forceinline__ void finish_distill(const Running& rest, const DistillArgs& a, int64_t row, int id, float value, bool ok,
-                                               Slots& slots) {
-  // rest: the sums over all tokens, or with tail over the unlisted ones
+__device__ __forceinline__ void finish_distill(const Running& rest, const DistillArgs& a, int64_t row, const TeacherSmem& sm) {
+  constexpr int kEntries = CAMERA_MAX_ALTERNATIVES / kWave;
+  const int lane = threadIdx.x;
   const double inv_t = 1.0 / (double)a.temperature;
-  const float z = ok ? Pack<T>::one(static_cast<const T*>(a.logits)[row * a.ld + id]) : -INFINITY;
+  bool ok[kEntries];
+  float z[kEntries], value[kEntries];
+  float z_max = -INFINITY, value_max = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < kEntries; ++e) {
+    const int j = e * kWave + lane;
+    ok[e] = j < a.teacher.k && entry_counts(sm, j, a.vocab);
+    z[e] = value[e] = -INFINITY;
+    if (ok[e]) {
+      z[e] = Pack<T>::one(static_cast<const T*>(a.logits)[row * a.ld + sm.id[j]]);
+      value[e] = sm.value[j];
+    }
+    z_max = fmaxf(z_max, z[e]);
+    value_max = fmaxf(value_max, value[e]);
+  }
   float m = rest.m;
-  double sum = rest.s;
+  double sum = rest.s, log_sum = 0.0, norm = 0.0;
   if (a.tail) {
-    m = fmaxf(m, block_all(z, Max{}, slots.f[0]));
+    m = fmaxf(m, wave_all(z_max, Max{}));
     const double ref = reference(m);
-    sum = block_all(z > -INFINITY ? exp(((double)z - ref) * inv_t) : 0.0, Add{}, slots.d);
+    double listed = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e)
+      if (z[e] > -INFINITY) listed += exp(((double)z[e] - ref) * inv_t);
+    sum = wave_all(listed, Add{});
     if (rest.m > -INFINITY) sum += (double)rest.s * exp(((double)rest.m - ref) * inv_t);
+  } else {
+    const double ref = reference(wave_all(value_max, Max{}));
+    double total = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e)
+      if (ok[e]) total += exp(((double)value[e] - ref) * inv_t);
+    total = wave_all(total, Add{});
+    if (total > 0.0) norm = ref * inv_t + log(total);
   }
-  const double log_sum = m == -INFINITY ? 0.0 : log(sum);
-  double norm = 0.0, log_q = value;
-  if (!a.tail) {
-    const float tm = block_all(ok ? value : -INFINITY, Max{}, slots.f[0]);
-    const double ref = reference(tm);
-    const double total = block_all(ok ? exp(((double)value - ref) * inv_t) : 0.0, Add{}, slots.d);
-    norm = total > 0.0 ? ref * inv_t + log(total) : 0.0;
-    log_q = (double)value * inv_t - norm;
-  }
-  const double q = ok ? exp(log_q) : 0.0;
-  const double log_p = z > -INFINITY ? ((double)z - (double)m) * inv_t - log_sum : -INFINITY;
-  double loss = block_all(q > 0.0 ? q * (log_q - log_p) : 0.0, Add{}, slots.d);
-  double mass = block_all(q, Add{}, slots.d), log_ratio = -INFINITY;
+  if (m > -INFINITY) log_sum = log(sum);
+  double loss = 0.0, mass = 0.0, log_ratio = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < kEntries; ++e)
+    if (ok[e]) {
+      const double log_q = a.tail ? (double)value[e] : (double)value[e] * inv_t - norm, q = exp(log_q);
+      const double log_p = z[e] > -INFINITY ? ((double)z[e] - (double)m) * inv_t - log_sum : -INFINITY;
+      mass += q;
+      if (q > 0.0) loss += q * (log_q - log_p);
+    }
+  loss = wave_all(loss, Add{});
+  mass = wave_all(mass, Add{});
   if (a.tail && rest.m > -INFINITY) {
     const double left = fmax(0.0, 1.0 - mass);
     const double log_rest = ((double)rest.m - (double)m) * inv_t + log((double)rest.s) - log_sum;
@@ -654,7 +707,7 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
       loss += left * log_ratio;
     }
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     a.loss[row] = (float)loss;
     float* st = a.stats + row * CAMERA_DISTILL_STATS;
     st[0] = m;
@@ -668,7 +721,7 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
 template <class T, bool TAIL>
 __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
   __shared__ Slots slots;
-  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  __shared__ TeacherSmem teacher;
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
@@ -677,36 +730,35 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
   const int len = (int)min(a.part_len, a.vocab - first);
   const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
   const float scale = kLog2e / a.temperature;
-  int id = -1;
-  float value = -INFINITY;
-  bool ok = false;
-  if (TAIL || a.parts == 1) ok = entry_counts(a.teacher, row, a.vocab, ids, &id, &value);
+  if (TAIL || a.parts == 1) load_teacher(a.teacher, row, teacher);
   Running mine;
   if constexpr (TAIL) {
     __shared__ __align__(16) uint32_t marks[kMaxListed / 32];
     for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
     __syncthreads();
-    if (ok && id >= first && id < first + len) atomicOr(&marks[(id - first) >> 5], 1u << ((id - first) & 31));
+    for (int j = threadIdx.x; j < a.teacher.k; j += kThreads) {
+      const int64_t at = teacher.id[j] - first;
+      if (at >= 0 && at < len && entry_counts(teacher, j, a.vocab)) atomicOr(&marks[at >> 5], 1u << (at & 31));
+    }
     __syncthreads();
     mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr);
   } else {
     mine = stream_part<T, false, false, false>(p, scale, nullptr, nullptr);
   }
   const Running r = block_running(mine, scale, slots);
-  if (a.parts == 1) finish_distill<T>(r, a, row, id, value, ok, slots);
-  else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, 0.0f, 0.0f);
+  if (a.parts == 1) {
+    if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
+  } else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, 0.0f, 0.0f);
 }
 template <class T>
 __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
   __shared__ Slots slots;
-  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  __shared__ TeacherSmem teacher;
   const int64_t row = linear_block();
   if (row >= a.n) return;
-  int id;
-  float value;
-  const bool ok = entry_counts(a.teacher, row, a.vocab, ids, &id, &value);
+  load_teacher(a.teacher, row, teacher);
   const Running r = join_parts(a.part_stats + row * a.parts, a.parts, kLog2e / a.temperature, slots);
-  finish_distill<T>(r, a, row, id, value, ok, slots);
+  if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
 }
 
 // d loss / dz_v = (mass p_v - q_v) / T for a listed v, p_v (mass - q_r / p_r) / T for an unlisted one (mass alone without tail):
@@ -715,7 +767,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
 template <class T>
 __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a, DistillTeacher teacher, int tail,
                                                                 const float* __restrict__ grad_loss) {
-  __shared__ int32_t ids[CAMERA_MAX_ALTERNATIVES];
+  __shared__ TeacherSmem list;
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
@@ -727,13 +779,14 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a,
     if (!p.accumulate) p.zero();
     return;
   }
-  int id;
-  float value;
-  const bool ok = entry_counts(teacher, row, a.vocab, ids, &id, &value);
-  const int64_t at = (int64_t)id - p.first;
-  const bool here = ok && at >= 0 && at < p.len;
+  load_teacher(teacher, row, list);
+  static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "a thread for every entry");
+  const int j = threadIdx.x;
+  const int64_t at = j < teacher.k ? list.id[j] - p.first : -1;
+  const bool here = at >= 0 && at < p.len && entry_counts(list, j, a.vocab);
   float listed = 0.0f;
   if (here) {
+    const float value = list.value[j];
     const float lp = fmaxf((Pack<T>::one(p.z[at]) - m) * inv_t - log_sum, kFloor);
     const float lq = tail ? value : value * inv_t - norm;
     listed = g * (mass * expf(lp) - expf(lq));
