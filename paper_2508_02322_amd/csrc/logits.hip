@@ -528,11 +528,10 @@ struct GradPart {
   int len;
   bool accumulate;
 
-  // out (+)= f(z, index in the part) over the part; f gets a vector's values and leaves the gradient in their place.
-  template <class F>
-  __device__ __forceinline__ void each(F&& f) const {
-    const int vecs = len / N, rest = len - vecs * N, tid = threadIdx.x;
-    Raw raw[kGradUnroll], old[kGradUnroll];
+  Raw raw[kGradUnroll], old[kGradUnroll];
+
+  __device__ __forceinline__ void fetch() {
+    const int vecs = len / N, tid = threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
       const int v = tid + u * kThreads;
@@ -541,6 +540,11 @@ struct GradPart {
         if (accumulate) old[u] = *reinterpret_cast<const Raw*>(out + v * N);
       }
     }
+  }
+  // out (+)= f(z, index in the part) over the part, after fetch(); f gets a vector's values and leaves the gradient in their place.
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    const int vecs = len / N, rest = len - vecs * N, tid = threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
       const int v = tid + u * kThreads;
@@ -591,7 +595,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
-  const GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
   const int64_t target = targets ? (int64_t)targets[row] : -1;
   const float m = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
   const float one = grad_logprob && target >= 0 && target < a.vocab ? grad_logprob[row] * a.inv_temperature : 0.0f;
@@ -602,6 +606,7 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a
   }
   const float inv_t = a.inv_temperature, h = two != 0.0f ? entropy[row] : 0.0f;
   const int64_t at = target - p.first;  // in this part, or not
+  p.fetch();
   p.each([&](float* x, int v, auto count) {
     constexpr int N = decltype(count)::value;
 #pragma unroll
@@ -624,24 +629,37 @@ __global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a
 // p_r is summed over the unlisted tokens themselves (1 - sum p_j would cancel): a bit per token of the part marks the listed ones.
 // The few values of the listed tokens are handled in float64.
 
-// A row's teacher list in LDS.  An entry counts if it names a token, has a probability and is the first to name its token.
+// A row's teacher list in LDS, id -1 where an entry does not count: it names no token, has no probability, or an entry before it
+// names the same token.
 struct TeacherSmem {
-  int32_t id[CAMERA_MAX_ALTERNATIVES];
+  __align__(16) int32_t id[CAMERA_MAX_ALTERNATIVES];
   float value[CAMERA_MAX_ALTERNATIVES];
 };
-__device__ __forceinline__ void load_teacher(const DistillTeacher& t, int64_t row, TeacherSmem& sm) {
-  for (int j = threadIdx.x; j < t.k; j += kThreads) {
-    sm.id[j] = t.idx[row * t.k + j];
-    sm.value[j] = t.logprob[row * t.k + j];
+__device__ __forceinline__ void load_teacher(const DistillTeacher& t, int64_t row, int64_t vocab, TeacherSmem& sm) {
+  static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "a thread for every entry");
+  const int j = threadIdx.x, padded = (t.k + 3) & ~3;
+  int32_t id = -1;
+  if (j < padded) {
+    float value = -INFINITY;
+    if (j < t.k) {
+      id = t.idx[row * t.k + j];
+      value = t.logprob[row * t.k + j];
+    }
+    sm.id[j] = id;
+    sm.value[j] = value;
+    if (id < 0 || id >= vocab || !(value > -INFINITY)) id = -1;
   }
   __syncthreads();
-}
-__device__ __forceinline__ bool entry_counts(const TeacherSmem& sm, int j, int64_t vocab) {
-  const int id = sm.id[j];
-  bool ok = id >= 0 && id < vocab && sm.value[j] > -INFINITY;
-  if (ok)
-    for (int i = 0; i < j; ++i) ok = ok && sm.id[i] != id;
-  return ok;
+  bool repeats = false;
+  if (j < padded) {
+    for (int i = 0; i < padded; i += 4) {  // whole vectors, no early end: the reads follow each other without waiting
+      const int4 other = *reinterpret_cast<const int4*>(&sm.id[i]);
+      repeats = repeats || (other.x == id && i < j) || (other.y == id && i + 1 < j) || (other.z == id && i + 2 < j) || (other.w == id && i + 3 < j);
+    }
+  }
+  __syncthreads();
+  if (j < padded && (repeats || id < 0)) sm.id[j] = -1;
+  __syncthreads();
 }
 
 // rest: the sums over all tokens, or with tail over the unlisted ones.  One wave does it, lane l the entries l, l + 64, ...: in
@@ -657,7 +675,7 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
 #pragma unroll
   for (int e = 0; e < kEntries; ++e) {
     const int j = e * kWave + lane;
-    ok[e] = j < a.teacher.k && entry_counts(sm, j, a.vocab);
+    ok[e] = j < a.teacher.k && sm.id[j] >= 0;
     z[e] = value[e] = -INFINITY;
     if (ok[e]) {
       z[e] = Pack<T>::one(static_cast<const T*>(a.logits)[row * a.ld + sm.id[j]]);
@@ -730,15 +748,15 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
   const int len = (int)min(a.part_len, a.vocab - first);
   const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
   const float scale = kLog2e / a.temperature;
-  if (TAIL || a.parts == 1) load_teacher(a.teacher, row, teacher);
+  if (TAIL || a.parts == 1) load_teacher(a.teacher, row, a.vocab, teacher);
   Running mine;
   if constexpr (TAIL) {
     __shared__ __align__(16) uint32_t marks[kMaxListed / 32];
     for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
     __syncthreads();
     for (int j = threadIdx.x; j < a.teacher.k; j += kThreads) {
-      const int64_t at = teacher.id[j] - first;
-      if (at >= 0 && at < len && entry_counts(teacher, j, a.vocab)) atomicOr(&marks[at >> 5], 1u << (at & 31));
+      const int64_t at = teacher.id[j] < 0 ? -1 : teacher.id[j] - first;
+      if (at >= 0 && at < len) atomicOr(&marks[at >> 5], 1u << (at & 31));
     }
     __syncthreads();
     mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr);
@@ -756,7 +774,7 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
   __shared__ TeacherSmem teacher;
   const int64_t row = linear_block();
   if (row >= a.n) return;
-  load_teacher(a.teacher, row, teacher);
+  load_teacher(a.teacher, row, a.vocab, teacher);
   const Running r = join_parts(a.part_stats + row * a.parts, a.parts, kLog2e / a.temperature, slots);
   if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
 }
@@ -771,7 +789,7 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a,
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
-  const GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
   const float* st = a.stats + row * CAMERA_DISTILL_STATS;
   const float m = st[0], log_sum = st[1], norm = st[2], mass = st[3], log_ratio = st[4];
   const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
@@ -779,11 +797,11 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a,
     if (!p.accumulate) p.zero();
     return;
   }
-  load_teacher(teacher, row, list);
-  static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "a thread for every entry");
+  p.fetch();  // in flight while the list is looked through
+  load_teacher(teacher, row, a.vocab, list);
   const int j = threadIdx.x;
-  const int64_t at = j < teacher.k ? list.id[j] - p.first : -1;
-  const bool here = at >= 0 && at < p.len && entry_counts(list, j, a.vocab);
+  const int64_t at = j < teacher.k && list.id[j] >= 0 ? list.id[j] - p.first : -1;
+  const bool here = at >= 0 && at < p.len;
   float listed = 0.0f;
   if (here) {
     const float value = list.value[j];
