@@ -178,8 +178,9 @@ struct RowPart {
 constexpr int kMaxListed = 1 << 18;  // elements of a part with marks: 32 KiB of LDS, four workgroups a compute unit
 
 // The thread's sums over its stripe.  cell_max (CELLS): upper half of the order bits of every cell's largest value, [cell][thread].
-template <class T, bool ENTROPY, bool LISTED, bool CELLS>
-__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks, uint16_t* cell_max) {
+// meanwhile(): done once the first loads are under way.
+template <class T, bool ENTROPY, bool LISTED, bool CELLS, class F>
+__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks, uint16_t* cell_max, F&& meanwhile) {
   constexpr int N = Pack<T>::N, U = kUnroll;
   const int tid = threadIdx.x;
   Running r;
@@ -196,10 +197,15 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
   float largest = -INFINITY;  // of the cell
   int cell = 0, groups = 0;
   int v = tid;
-  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads) {
-    typename Pack<T>::Raw raw[U];
+  typename Pack<T>::Raw raw[U];
+  auto fetch = [&] {
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = p.load(v + u * kThreads);
+    for (int u = 0; u < U; ++u)
+      if (v + u * kThreads < p.vecs) raw[u] = p.load(v + u * kThreads);
+  };
+  fetch();
+  meanwhile();
+  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads, fetch()) {
     float z[U * N];
 #pragma unroll
     for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
@@ -212,13 +218,8 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
       }
     }
   }
-  // up to three vectors more, their loads in flight together: one by one they took a latency each
-  typename Pack<T>::Raw raw[U - 1];
 #pragma unroll
-  for (int u = 0; u < U - 1; ++u)
-    if (v + u * kThreads < p.vecs) raw[u] = p.load(v + u * kThreads);
-#pragma unroll
-  for (int u = 0; u < U - 1; ++u)
+  for (int u = 0; u < U - 1; ++u)  // up to three vectors are left
     if (v + u * kThreads < p.vecs) {
       float z[N];
       one(raw[u], v + u * kThreads, z);
@@ -466,7 +467,7 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(LogprobArgs a) {
     __shared__ SelectSmem sm;
     select = &sm;
   }
-  const Running mine = stream_part<T, true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr);
+  const Running mine = stream_part<T, true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr, [] {});
   const Running r = block_running(mine, scale, slots);
   if (a.parts == 1) finish_logprobs<T>(r, a, row);
   else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
@@ -748,20 +749,22 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
   const int len = (int)min(a.part_len, a.vocab - first);
   const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
   const float scale = kLog2e / a.temperature;
-  if (TAIL || a.parts == 1) load_teacher(a.teacher, row, a.vocab, teacher);
   Running mine;
   if constexpr (TAIL) {
     __shared__ __align__(16) uint32_t marks[kMaxListed / 32];
-    for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.teacher.k; j += kThreads) {
-      const int64_t at = teacher.id[j] < 0 ? -1 : teacher.id[j] - first;
-      if (at >= 0 && at < len) atomicOr(&marks[at >> 5], 1u << (at & 31));
-    }
-    __syncthreads();
-    mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr);
+    mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr, [&] {
+      for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
+      load_teacher(a.teacher, row, a.vocab, teacher);
+      for (int j = threadIdx.x; j < a.teacher.k; j += kThreads) {
+        const int64_t at = teacher.id[j] < 0 ? -1 : teacher.id[j] - first;
+        if (at >= 0 && at < len) atomicOr(&marks[at >> 5], 1u << (at & 31));
+      }
+      __syncthreads();
+    });
   } else {
-    mine = stream_part<T, false, false, false>(p, scale, nullptr, nullptr);
+    mine = stream_part<T, false, false, false>(p, scale, nullptr, nullptr, [&] {
+      if (a.parts == 1) load_teacher(a.teacher, row, a.vocab, teacher);
+    });
   }
   const Running r = block_running(mine, scale, slots);
   if (a.parts == 1) {
