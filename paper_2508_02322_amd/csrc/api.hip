@@ -1234,39 +1234,55 @@ int check_gated(camera_ctx* ctx, const void* X, int dtype, int64_t n, int64_t d_
   if (d_ff < 1 || d_ff > (1 << 24)) return fail(ctx, CAMERA_ESHAPE, "d_ff: must be in [1, 2^24]");
   if (W_gate == nullptr || W_up == nullptr) return fail(ctx, CAMERA_EINVAL, "W_gate / W_up: NULL");
   if (!aligned16(W_gate) || !aligned16(W_up)) return fail(ctx, CAMERA_ESHAPE, "W_gate / W_up: not 16-byte aligned");
-  const int tile_m = camera::gemm_tile_m(dtype, d_ff);
-  if (up_to(n, tile_m) / tile_m > 65535 || 2 * up_to(d_ff, tile_m) / tile_m > 65535 || n >= int64_t(1) << 30)
+  if (camera::group_tiles(dtype, 1, n, d_ff).tiles > 65535 || camera::group_tiles(dtype, 2, d_ff, d_model / 2).tiles > 65535)
     return fail(ctx, CAMERA_EUNSUPPORTED, "n / d_ff: too large for one call");
   return CAMERA_OK;
 }
-// The tables of `groups` groups of `rows` left-operand rows each, all of them in order.
-struct DenseTables {
-  BucketPlan plan;
-  int groups = 0, tile_m = 0, max_tiles = 0;
-  int64_t rows = 0;
-  void take(Carver& cv, int groups_, int64_t rows_, int tile_m_) {
-    groups = groups_;
-    rows = rows_;
-    tile_m = tile_m_;
-    max_tiles = (int)(groups * ((rows + tile_m - 1) / tile_m));
-    plan.take(cv, true, false, groups, groups * rows, max_tiles, 0);
+// H and / or the projections of every token.  Up to kGatedRowsMost bf16 tokens the weights stream straight into operands.
+int gated_projections(camera_ctx* ctx, hipStream_t stream, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
+                      const void* W_gate, const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre) {
+  const int64_t pre_ld = up_to(d_ff, 8);
+  Bracket b(ctx, stream, CAMERA_K_GEMM);
+  if (dtype == CAMERA_BF16 && n <= camera::kGatedRowsMost) {
+    CAMERA_HIP(camera::launch_gated_rows(stream, X, ldx, n, d_model, W_gate, W_up, d_ff, H, ldh, pre, pre_ld), "gated rows launch");
+    return CAMERA_OK;
   }
-};
-// H and / or the projections of every token by the tiled contraction.
-int gated_projections(camera_ctx* ctx, hipStream_t stream, const void* X, int dtype, int64_t d_model, int64_t ldx, const void* W_gate,
-                      const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre, const DenseTables& dense) {
-  const camera::BucketTables t = dense.plan.bind(static_cast<char*>(ctx->ws), ctx->zeros);
-  CAMERA_HIP(camera::launch_dense_tables(stream, dense.rows, dense.groups, dense.tile_m, dense.max_tiles, t), "dense tables launch");
+  const camera::GroupTiles tiles = camera::group_tiles(dtype, 1, n, d_ff);
+  camera::BucketTables t{};
+  t.zeros = ctx->zeros;
   camera::GemmEpilogue ep;
   ep.mode = camera::GemmEpilogue::kGated;
+  ep.group_rows = (int)n;
+  ep.small_tiles = tiles.small;
   ep.hidden = H;
   ep.ld_hidden = ldh;
   ep.product = pre;
-  ep.col_gap = (int)up_to(d_ff, 8);
-  ep.ld_product = 2 * ep.col_gap;
-  Bracket b(ctx, stream, CAMERA_K_GEMM);
-  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, X, ldx, d_model, d_ff, 1, W_gate, W_up, 0, dense.max_tiles, t, ep),
+  ep.col_gap = (int)pre_ld;
+  ep.ld_product = 2 * pre_ld;
+  ep.stream_product = camera::product_streams(n, 2 * pre_ld);
+  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, X, ldx, d_model, d_ff, 1, W_gate, W_up, 0, (int)tiles.tiles, t, ep),
              "gated projections launch");
+  return CAMERA_OK;
+}
+// out[e][r][c] = left row e * rows + r times column c of the right matrix, whose d_model columns are given as rows: [d_model][k].
+int gated_product(camera_ctx* ctx, hipStream_t stream, int dtype, int groups, int64_t rows, int64_t k, const void* left, const void* right,
+                  int64_t d_model, void* out, int64_t ld_out, int64_t expert_gap) {
+  const int64_t half = d_model / 2;
+  const camera::GroupTiles tiles = camera::group_tiles(dtype, groups, rows, half);
+  camera::BucketTables t{};
+  t.zeros = ctx->zeros;
+  camera::GemmEpilogue ep;
+  ep.mode = camera::GemmEpilogue::kRounded;
+  ep.group_rows = (int)rows;
+  ep.small_tiles = tiles.small;
+  ep.rounded = out;
+  ep.ld_product = ld_out;
+  ep.col_gap = (int)half;
+  ep.expert_gap = expert_gap;
+  const size_t es = dtype == CAMERA_BF16 ? 2 : 4;
+  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, left, k, k, half, groups, right, static_cast<const char*>(right) + es * half * k, 0,
+                                         (int)tiles.tiles, t, ep),
+             "gated product launch");
   return CAMERA_OK;
 }
 }  // namespace
@@ -1281,13 +1297,10 @@ int camera_gated_ffn(camera_ctx* ctx, void* stream_, const void* X, int dtype, i
   if (!aligned16(H) || !aligned16(pre)) return fail(ctx, CAMERA_ESHAPE, "H / pre: not 16-byte aligned");
   if (n == 0) return CAMERA_OK;
 
-  Carver cv;
-  DenseTables dense;
-  dense.take(cv, 1, n, camera::gemm_tile_m(dtype, d_ff));
   DeviceGuard guard;
   CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
-  if (int rc = ensure_workspace(ctx, cv.used)) return rc;
-  return gated_projections(ctx, static_cast<hipStream_t>(stream_), X, dtype, d_model, ldx, W_gate, W_up, d_ff, H, ldh, pre, dense);
+  if (int rc = ensure_workspace(ctx, 0)) return rc;  // the zero page
+  return gated_projections(ctx, static_cast<hipStream_t>(stream_), X, dtype, n, d_model, ldx, W_gate, W_up, d_ff, H, ldh, pre);
 }
 
 int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
@@ -1307,13 +1320,8 @@ int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int
   const bool weights = dW_gate != nullptr || dW_up != nullptr;
   if (!weights && (dX == nullptr || n == 0)) return CAMERA_OK;
 
-  const int tile_m = camera::gemm_tile_m(dtype, d_ff);
-  const int64_t f_pad = up_to(d_ff, 64), n_pad = up_to(n, 64), half = d_model / 2;
-  const int64_t pre_ld = up_to(d_ff, 8);
+  const int64_t f_pad = up_to(d_ff, 64), n_pad = up_to(n, 64), pre_ld = up_to(d_ff, 8);
   Carver cv;
-  DenseTables by_token, by_channel;
-  by_token.take(cv, 1, n, tile_m);
-  by_channel.take(cv, 2, d_ff, tile_m);
   const size_t o_pre = cv.take(pre == nullptr ? sizeof(float) * n * 2 * pre_ld : 0);
   const size_t o_rows = cv.take(dX != nullptr ? es * n * 2 * f_pad : 0);
   const size_t o_wt = cv.take(dX != nullptr ? es * d_model * 2 * f_pad : 0);
@@ -1331,50 +1339,27 @@ int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int
   char* ws = static_cast<char*>(ctx->ws);
   if (pre == nullptr) {
     float* made = reinterpret_cast<float*>(ws + o_pre);
-    if (int rc = gated_projections(ctx, stream, X, dtype, d_model, ldx, W_gate, W_up, d_ff, nullptr, 0, made, by_token)) return rc;
+    if (int rc = gated_projections(ctx, stream, X, dtype, n, d_model, ldx, W_gate, W_up, d_ff, nullptr, 0, made)) return rc;
     pre = made;
   }
   {
     Bracket b(ctx, stream, CAMERA_K_GATED_GRAD);
-    CAMERA_HIP(camera::launch_gated_grad(stream, dtype, pre, pre_ld, dH, lddh, n, d_ff, dX != nullptr ? ws + o_rows : nullptr, f_pad,
-                                         weights ? ws + o_cols : nullptr, n_pad),
-               "gated gradient launch");
-    if (dX != nullptr) {
-      CAMERA_HIP(camera::launch_transpose(stream, dtype, W_gate, d_ff, d_model, d_model, ws + o_wt, 2 * f_pad, f_pad), "transpose launch");
-      CAMERA_HIP(camera::launch_transpose(stream, dtype, W_up, d_ff, d_model, d_model, ws + o_wt + es * f_pad, 2 * f_pad, f_pad),
-                 "transpose launch");
-    }
-    if (weights) CAMERA_HIP(camera::launch_transpose(stream, dtype, X, n, d_model, ldx, ws + o_xt, n_pad, n_pad), "transpose launch");
+    const camera::GatedOperands a{pre, pre_ld, dH, X, W_gate, W_up, lddh, ldx, n, d_model, d_ff, f_pad, n_pad,
+                                  dX != nullptr ? ws + o_rows : nullptr, weights ? ws + o_cols : nullptr,
+                                  dX != nullptr ? ws + o_wt : nullptr, weights ? ws + o_xt : nullptr};
+    CAMERA_HIP(camera::launch_gated_operands(stream, dtype, a), "gated operands launch");
   }
   Bracket b(ctx, stream, CAMERA_K_GEMM);
-  if (dX != nullptr) {  // [dG | dU] times [W_gate; W_up]: the columns of dX in two halves
-    const camera::BucketTables t = by_token.plan.bind(ws, ctx->zeros);
-    CAMERA_HIP(camera::launch_dense_tables(stream, n, 1, tile_m, by_token.max_tiles, t), "dense tables launch");
-    camera::GemmEpilogue ep;
-    ep.mode = camera::GemmEpilogue::kRounded;
-    ep.rounded = dX;
-    ep.ld_product = lddx;
-    ep.col_gap = (int)half;
-    CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, ws + o_rows, 2 * f_pad, 2 * f_pad, half, 1, ws + o_wt,
-                                           ws + o_wt + es * half * 2 * f_pad, 0, by_token.max_tiles, t, ep),
-               "input gradient launch");
-  }
+  if (dX != nullptr)  // [dG | dU] times [W_gate; W_up]
+    if (int rc = gated_product(ctx, stream, dtype, 1, n, 2 * f_pad, ws + o_rows, ws + o_wt, d_model, dX, lddx, 0)) return rc;
   if (weights) {  // two groups of left rows, dG^T and dU^T, or one of them
     const bool both = dW_gate != nullptr && dW_up != nullptr;
-    const int groups = both ? 2 : 1, max_tiles = both ? by_channel.max_tiles : by_channel.max_tiles / 2;
     const char* left = ws + o_cols + (dW_gate == nullptr ? es * d_ff * n_pad : 0);
-    const camera::BucketTables t = by_channel.plan.bind(ws, ctx->zeros);
-    CAMERA_HIP(camera::launch_dense_tables(stream, d_ff, groups, tile_m, max_tiles, t), "dense tables launch");
-    camera::GemmEpilogue ep;
-    ep.mode = camera::GemmEpilogue::kRounded;
-    ep.rounded = dW_gate != nullptr ? dW_gate : dW_up;
-    ep.ld_product = d_model;
-    ep.col_gap = (int)half;
-    if (both)  // group 1 continues behind group 0's rows: bring it to its own matrix
-      ep.expert_gap = (int64_t)(reinterpret_cast<intptr_t>(dW_up) - reinterpret_cast<intptr_t>(dW_gate)) / (int64_t)es - d_ff * d_model;
-    CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, left, n_pad, n_pad, half, groups, ws + o_xt, ws + o_xt + es * half * n_pad, 0,
-                                           max_tiles, t, ep),
-               "weight gradient launch");
+    // group 1 continues behind group 0's rows: bring it to its own matrix
+    const int64_t gap = !both ? 0 : (reinterpret_cast<intptr_t>(dW_up) - reinterpret_cast<intptr_t>(dW_gate)) / (int64_t)es - d_ff * d_model;
+    if (int rc = gated_product(ctx, stream, dtype, both ? 2 : 1, d_ff, n_pad, left, ws + o_xt, d_model, dW_gate != nullptr ? dW_gate : dW_up,
+                               d_model, gap))
+      return rc;
   }
   return CAMERA_OK;
 }

@@ -89,7 +89,19 @@ struct GemmEpilogue {
   int64_t ld_hidden = 0;
   void* rounded = nullptr;
   int64_t expert_gap = 0;
+  // kGated, kRounded: n_experts groups of group_rows left rows, one behind the other, cut as group_tiles says; of the bucket
+  // tables only `zeros` is read
+  int group_rows = 0;
+  bool small_tiles = false;
 };
+// How the left rows of those two are cut: tile height, tiles in all (max_tiles of the launch), and whether in small tiles.
+struct GroupTiles {
+  int tile_m = 0;
+  bool small = false;
+  int64_t tiles = 0;
+};
+constexpr int kSmallTilesBelow = 256;
+GroupTiles group_tiles(int dtype, int groups, int64_t rows, int64_t d_ff);
 hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int64_t ldx, int64_t d_model,
                                int64_t d_ff, int n_experts, const void* W_gate, const void* W_up,
                                int64_t stride_gu, int max_tiles, const BucketTables& t, const GemmEpilogue& ep);
@@ -314,15 +326,23 @@ hipError_t launch_distill_grad(hipStream_t stream, int dtype, const LogitGradArg
                                const float* grad_loss);
 
 // ---- gated.hip --------------------------------------------------------------
-// From G, U (pre: float32 [n][2][pre_ld]) and dH: dG = dH U silu'(G) and dU = dH silu(G) in the inputs' type, as rows
-// rows_out [n][2][f_pad] and transposed cols_out [2][d_ff][n_pad], zero in the padding (f_pad, n_pad: multiples of 64).  Either
-// output may be NULL.
-hipError_t launch_gated_grad(hipStream_t stream, int dtype, const float* pre, int64_t pre_ld, const void* dH, int64_t lddh, int64_t n,
-                             int64_t d_ff, void* rows_out, int64_t f_pad, void* cols_out, int64_t n_pad);
-// dst[c][r] = src[r][c] for r < rows, zero for rows <= r < rows_pad (a multiple of 64); cols a multiple of 4.
-hipError_t launch_transpose(hipStream_t stream, int dtype, const void* src, int64_t rows, int64_t cols, int64_t lds, void* dst,
-                            int64_t ldd, int64_t rows_pad);
+// What the backward pass of the gated block makes for its products, in one launch.  From G, U (pre: float32 [n][2][pre_ld]) and dH:
+// dG = dH U silu'(G) and dU = dH silu(G) in the inputs' type, as rows [n][2][f_pad] and transposed, cols [2][d_ff][n_pad]; the
+// transposed matrices w_t [d_model][2][f_pad] (gate, up) and x_t [d_model][n_pad].  Zero in the padding (f_pad, n_pad: multiples of
+// 64).  rows and w_t, and cols and x_t, may be NULL.
+struct GatedOperands {
+  const float* pre;
+  int64_t pre_ld;
+  const void *dH, *X, *W_gate, *W_up;
+  int64_t lddh, ldx, n, d_model, d_ff, f_pad, n_pad;
+  void *rows, *cols, *w_t, *x_t;
+};
+hipError_t launch_gated_operands(hipStream_t stream, int dtype, const GatedOperands& a);
 // vectors of 16 bytes set to zero
 hipError_t launch_zero(hipStream_t stream, void* dst, int64_t vectors);
+// H and / or pre of up to kGatedRowsMost tokens, bf16: every weight row is read once, straight into matrix operands.
+constexpr int kGatedRowsMost = 64;
+hipError_t launch_gated_rows(hipStream_t stream, const void* X, int64_t ldx, int64_t n, int64_t d_model, const void* W_gate,
+                             const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre, int64_t pre_ld);
 
 }  // namespace camera

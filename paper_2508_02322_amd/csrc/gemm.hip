@@ -108,6 +108,8 @@ constexpr int kChunkM = 4;     // otherwise this many
 enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3, kEpiGated = 4, kEpiRounded = 5 };
 constexpr bool epi_hidden(int epi) { return epi == kEpiHidden || epi == kEpiListed; }
 constexpr bool epi_by_slot(int epi) { return epi == kEpiProduct || epi == kEpiRounded; }  // token rows = bucket slots
+// These two have groups of ep.group_rows left rows each, one behind the other, and no bucket tables.
+constexpr bool epi_plain(int epi) { return epi == kEpiGated || epi == kEpiRounded; }
 struct EpiArgs {
   float* part_phi2;
   float* part_max;
@@ -127,6 +129,7 @@ struct EpiArgs {
   int64_t blocks;          // workgroups, where not every token tile there may be has one for every part (host)
   void* rounded;           // kEpiRounded: row stride ld_product
   int64_t expert_gap;
+  int group_rows;          // kEpiGated, kEpiRounded
 };
 
 // One wave instruction of the direct global -> LDS path: lane l's 16 bytes at p (+ IMM) go to LDS bytes
@@ -663,8 +666,13 @@ __device__ __forceinline__ void tile_body16(const TileState<C>& st, int n0, int 
             }
             if (ep.product != nullptr) {
               float* dst = ep.product + (int64_t)(st.row_first + row) * ep.ld_product + col0;
-              *reinterpret_cast<f32x4*>(dst) = g;
-              *reinterpret_cast<f32x4*>(dst + ep.col_gap) = u;
+              if (ep.stream_product) {
+                __builtin_nontemporal_store(g, reinterpret_cast<f32x4*>(dst));
+                __builtin_nontemporal_store(u, reinterpret_cast<f32x4*>(dst + ep.col_gap));
+              } else {
+                *reinterpret_cast<f32x4*>(dst) = g;
+                *reinterpret_cast<f32x4*>(dst + ep.col_gap) = u;
+              }
             }
           }
     }
@@ -950,7 +958,16 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void grouped_gemm_bf
   // memory-side cache instead of HBM, and an expert's weights leave HBM once), then the tiles of
   // the chunk.
   const int n_tiles_n = (d_ff + BN - 1) / BN;
-  const int total = tile_offset[n_experts] * n_tiles_n;
+  [[maybe_unused]] const int group_tiles = epi_plain(EPI) ? (ep.group_rows + BM - 1) / BM : 0;
+  auto first_tile = [&](int e) {
+    if constexpr (epi_plain(EPI)) return e * group_tiles;
+    else return tile_offset[e];
+  };
+  auto first_row = [&](int e) {
+    if constexpr (epi_plain(EPI)) return e * ep.group_rows;
+    else return offsets[e];
+  };
+  const int total = first_tile(n_experts) * n_tiles_n;
   const int per_xcd = (total + kXcds - 1) / kXcds;
   const int block = linear_block();
   int seq = block / kXcds;
@@ -972,9 +989,11 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void grouped_gemm_bf
   }
   const int logical = first + seq;
   if (seq >= per_xcd || logical >= total) return;  // block-uniform: nothing here
-  const int e = tile_expert[logical / n_tiles_n];  // expert e owns logical ids tile_offset[e] * n_tiles_n ..
-  const int m_e = tile_offset[e + 1] - tile_offset[e];
-  const int local = logical - tile_offset[e] * n_tiles_n;
+  int e;  // expert e owns logical ids first_tile(e) * n_tiles_n ..
+  if constexpr (epi_plain(EPI)) e = logical / (group_tiles * n_tiles_n);
+  else e = tile_expert[logical / n_tiles_n];
+  const int m_e = first_tile(e + 1) - first_tile(e);
+  const int local = logical - first_tile(e) * n_tiles_n;
   const int chunk_m = m_e <= kChunkMax ? m_e : kChunkM;       // M-tiles that run side by side
   const int group_n = max(1, kPatch / chunk_m);               // N-tiles that run side by side
   const int group = local / (m_e * group_n);                  // all groups but the last are full
@@ -984,10 +1003,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void grouped_gemm_bf
   const int chunk_h = min(chunk_m, m_e - chunk * chunk_m);
   const int in_chunk = in_group - chunk * chunk_m * group_w;
   const int tile_n = group * group_n + in_chunk / chunk_h;
-  const int slot = tile_offset[e] + chunk * chunk_m + in_chunk % chunk_h;
-  const int tile_in_expert = slot - tile_offset[e];
-  const int row_first = offsets[e] + tile_in_expert * BM;  // first bucket slot of this tile
-  const int m_len = min(BM, offsets[e + 1] - row_first);   // >= 1
+  const int slot = first_tile(e) + chunk * chunk_m + in_chunk % chunk_h;
+  const int tile_in_expert = slot - first_tile(e);
+  const int row_first = first_row(e) + tile_in_expert * BM;  // first bucket slot of this tile
+  const int m_len = min(BM, first_row(e + 1) - row_first);   // >= 1
   const int n0 = tile_n * BN;
 
   TileWork w;
@@ -1302,19 +1321,30 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
   // Workgroup -> tile: every XCD runs a contiguous run of logical ids (see grouped_gemm_bf16_kernel), ordered expert,
   // N-tile, M-tile, so that the M-tiles that read the same weight rows run side by side on one L2.
   const int n_tiles_n = (d_ff + F32_BN - 1) / F32_BN;
-  const int total = tile_offset[n_experts] * n_tiles_n;
+  [[maybe_unused]] const int group_tiles = epi_plain(EPI) ? (ep.group_rows + F32_BM - 1) / F32_BM : 0;
+  auto first_tile = [&](int e) {
+    if constexpr (epi_plain(EPI)) return e * group_tiles;
+    else return tile_offset[e];
+  };
+  auto first_row = [&](int e) {
+    if constexpr (epi_plain(EPI)) return e * ep.group_rows;
+    else return offsets[e];
+  };
+  const int total = first_tile(n_experts) * n_tiles_n;
   const int per_xcd = (total + kXcds - 1) / kXcds;
   const int block = linear_block();
   const int seq = block / kXcds;
   const int logical = (block % kXcds) * per_xcd + seq;
   if (seq >= per_xcd || logical >= total) return;
-  const int e = tile_expert[logical / n_tiles_n];
-  const int m_e = tile_offset[e + 1] - tile_offset[e];
-  const int local = logical - tile_offset[e] * n_tiles_n;
+  int e;
+  if constexpr (epi_plain(EPI)) e = logical / (group_tiles * n_tiles_n);
+  else e = tile_expert[logical / n_tiles_n];
+  const int m_e = first_tile(e + 1) - first_tile(e);
+  const int local = logical - first_tile(e) * n_tiles_n;
   const int tile_in_expert = local % m_e;
-  const int slot = tile_offset[e] + tile_in_expert;
-  const int row_first = offsets[e] + tile_in_expert * F32_BM;
-  const int m_len = min(F32_BM, offsets[e + 1] - row_first);  // >= 1
+  const int slot = first_tile(e) + tile_in_expert;
+  const int row_first = first_row(e) + tile_in_expert * F32_BM;
+  const int m_len = min(F32_BM, first_row(e + 1) - row_first);  // >= 1
   const int n0 = local / m_e * F32_BN;
 
   __shared__ __align__(16) float s_x[F32_BM * kF32Row];
@@ -1339,7 +1369,7 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
     const int rr = row_first + (row < m_len ? row : 0);
     int64_t tok;
     if constexpr (epi_by_slot(EPI)) tok = rr;  // the left operand is indexed by bucket slot
-    else tok = perm ? perm[rr] : rr - offsets[e];
+    else tok = perm ? perm[rr] : rr - first_row(e);
     x_src[p] = X + tok * ldx + lk;
   }
   const int64_t w_off = (int64_t)e * stride_gu + (int64_t)min(n0 + lrow, d_ff - 1) * d_model + lk;
@@ -1528,6 +1558,9 @@ __global__ __launch_bounds__(256) void zero_hidden_kernel(const int32_t* __restr
 using Bf16Cfg = GemmCfg<2, 2, 4, 2, 64, 2, 3>;
 static_assert(Bf16Cfg::BM == kPlanTileM && Bf16Cfg::BN == kPlanTileN && Bf16Cfg::KT == kPlanTileK && kXcds == kPlanDies, "the plan's tile");
 
+// For products of few tiles: two waves of 32 x 64 x {gate, up}, three workgroups a compute unit.
+using SmallCfg = GemmCfg<2, 1, 1, 2, 64, 2, 2>;
+
 // Whether the scalar-base form of the tile loads can address the operands: 32-bit byte offsets from the start of
 // the token matrix (a_rows rows of lda elements) and of one expert's weight matrix (b_rows rows of ldw elements).
 // Kept below 2 GiB, where the offset reads the same as a signed and as an unsigned number.
@@ -1537,6 +1570,18 @@ bool fits_32bit_offsets(int64_t a_rows, int64_t lda, int64_t b_rows, int64_t ldw
 }
 
 }  // namespace
+
+GroupTiles group_tiles(int dtype, int groups, int64_t rows, int64_t d_ff) {
+  GroupTiles g;
+  g.tile_m = dtype == CAMERA_BF16 ? Bf16Cfg::BM : F32_BM;
+  const int64_t columns = (d_ff + Bf16Cfg::BN - 1) / Bf16Cfg::BN;
+  if (dtype == CAMERA_BF16 && groups * ((rows + Bf16Cfg::BM - 1) / Bf16Cfg::BM) * columns < kSmallTilesBelow) {
+    g.small = true;
+    g.tile_m = SmallCfg::BM;
+  }
+  g.tiles = groups * ((rows + g.tile_m - 1) / g.tile_m);
+  return g;
+}
 
 int gemm_tile_m(int dtype, int64_t d_ff) {
   (void)d_ff;
@@ -1550,11 +1595,10 @@ static hipError_t allow_lds(OncePerDevice& once, const void* kernel, int bytes) 
   return once(device, [&] { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
 }
 
-template <int EPI>
+template <int EPI, class C = Bf16Cfg>
 static hipError_t launch_bf16(hipStream_t stream, const void* X, int64_t ldx, int64_t d_model, int64_t d_ff,
                               int n_experts, const void* W_gate, const void* W_up, int64_t stride_gu, int max_tiles,
                               const BucketTables& t, const EpiArgs& ep) {
-  using C = Bf16Cfg;
   // token rows lie below max_tiles * BM (every token, and every bucket slot, belongs to some tile)
   const bool tail = d_model % C::KT != 0 || !fits_32bit_offsets((int64_t)max_tiles * C::BM, ldx, d_ff, d_model);
   auto kern = tail ? grouped_gemm_bf16_kernel<C, true, EPI> : grouped_gemm_bf16_kernel<C, false, EPI>;
@@ -1577,7 +1621,7 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
                                int64_t stride_gu, int max_tiles, const BucketTables& t, const GemmEpilogue& e) {
   if (max_tiles <= 0) return hipSuccess;
   EpiArgs ep{e.part_phi2, e.part_max, e.hidden, e.keep, nullptr, e.product, e.ld_product, e.col_gap, d_ff, 0, e.stream_product ? 1 : 0,
-             e.split_plan.most_parts, e.part_stride, e.split, e.parts, e.split_plan.blocks, e.rounded, e.expert_gap};
+             e.split_plan.most_parts, e.part_stride, e.split, e.parts, e.split_plan.blocks, e.rounded, e.expert_gap, e.group_rows};
   if (e.mode == GemmEpilogue::kGated) {
     ep.ld_hidden = e.ld_hidden;
     ep.pad_hidden = dtype == CAMERA_BF16 ? 8 : 4;
@@ -1592,9 +1636,11 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
       case GemmEpilogue::kProduct:
         return launch_bf16<kEpiProduct>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kGated:
-        return launch_bf16<kEpiGated>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
+        return (e.small_tiles ? launch_bf16<kEpiGated, SmallCfg> : launch_bf16<kEpiGated>)(stream, X, ldx, d_model, d_ff, n_experts, W_gate,
+                                                                                          W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kRounded:
-        return launch_bf16<kEpiRounded>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
+        return (e.small_tiles ? launch_bf16<kEpiRounded, SmallCfg> : launch_bf16<kEpiRounded>)(stream, X, ldx, d_model, d_ff, n_experts,
+                                                                                               W_gate, W_up, stride_gu, max_tiles, t, ep);
       default:
         return hipErrorInvalidValue;
     }
