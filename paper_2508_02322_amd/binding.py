@@ -103,9 +103,10 @@ def _check_matrix(t, name: str, like=None):
     """[rows, cols] with unit inner stride (the row stride is passed on)."""
     if t is None:
         return
-    _require(t.dim() == 2 and t.stride(1) == 1, f"{name}: must be 2-D with unit inner stride (got strides {tuple(t.stride())})")
-    if like is not None:
-        _require(t.dtype == like.dtype and t.device == like.device, f"{name}: dtype / device differ from X")
+    if t.dim() != 2 or t.stride(1) != 1:
+        _require(False, f"{name}: must be 2-D with unit inner stride (got strides {tuple(t.stride())})")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _require(False, f"{name}: dtype / device differ from X")
 
 
 def _check_experts(t, name: str, like=None):
@@ -121,11 +122,12 @@ def _check_experts(t, name: str, like=None):
 def _check_flat(t, name: str, dtype=None, device=None):
     if t is None:
         return
-    _require(t.is_contiguous(), f"{name}: must be contiguous")
-    if dtype is not None:
-        _require(t.dtype == dtype, f"{name}: must be {dtype}")
-    if device is not None:
-        _require(t.device == device, f"{name}: on another device")
+    if not t.is_contiguous():
+        _require(False, f"{name}: must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        _require(False, f"{name}: must be {dtype}")
+    if device is not None and t.device != device:
+        _require(False, f"{name}: on another device")
 
 
 def _row_stride(t) -> int:
@@ -391,7 +393,8 @@ class Camera:
             if t is None:
                 continue
             _check_flat(t, name, dtype, logits.device)
-            _require(tuple(t.shape) == shape, f"{name}: must be {list(shape)} (got {list(t.shape)})")
+            if t.shape != shape:
+                _require(False, f"{name}: must be {list(shape)} (got {list(t.shape)})")
 
     def _gradient_rows(self, logits, dlogits, accumulate):
         if dlogits is None:

@@ -1234,55 +1234,67 @@ int check_gated(camera_ctx* ctx, const void* X, int dtype, int64_t n, int64_t d_
   if (d_ff < 1 || d_ff > (1 << 24)) return fail(ctx, CAMERA_ESHAPE, "d_ff: must be in [1, 2^24]");
   if (W_gate == nullptr || W_up == nullptr) return fail(ctx, CAMERA_EINVAL, "W_gate / W_up: NULL");
   if (!aligned16(W_gate) || !aligned16(W_up)) return fail(ctx, CAMERA_ESHAPE, "W_gate / W_up: not 16-byte aligned");
-  if (camera::group_tiles(dtype, 1, n, d_ff).tiles > 65535 || camera::group_tiles(dtype, 2, d_ff, d_model / 2).tiles > 65535)
+  const int64_t tile_m = dtype == CAMERA_BF16 ? camera::kPlanTileM : camera::kPlanF32M;
+  if (up_to(n, tile_m) / tile_m > 65535 || 2 * up_to(d_ff, tile_m) / tile_m > 65535)
     return fail(ctx, CAMERA_EUNSUPPORTED, "n / d_ff: too large for one call");
   return CAMERA_OK;
 }
-// H and / or the projections of every token.  Up to kGatedRowsMost bf16 tokens the weights stream straight into operands.
+// H and / or the projections of every token.
 int gated_projections(camera_ctx* ctx, hipStream_t stream, const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,
                       const void* W_gate, const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre) {
   const int64_t pre_ld = up_to(d_ff, 8);
   Bracket b(ctx, stream, CAMERA_K_GEMM);
-  if (dtype == CAMERA_BF16 && n <= camera::kGatedRowsMost) {
+  if (dtype == CAMERA_BF16 && camera::gated_by_rows(n, d_ff)) {
     CAMERA_HIP(camera::launch_gated_rows(stream, X, ldx, n, d_model, W_gate, W_up, d_ff, H, ldh, pre, pre_ld), "gated rows launch");
     return CAMERA_OK;
   }
-  const camera::GroupTiles tiles = camera::group_tiles(dtype, 1, n, d_ff);
+  const camera::GroupPlan plan = camera::group_plan(dtype == CAMERA_BF16, 1, n, d_ff, d_model, 1);
   camera::BucketTables t{};
   t.zeros = ctx->zeros;
   camera::GemmEpilogue ep;
   ep.mode = camera::GemmEpilogue::kGated;
   ep.group_rows = (int)n;
-  ep.small_tiles = tiles.small;
+  ep.small_tiles = plan.small;
   ep.hidden = H;
   ep.ld_hidden = ldh;
   ep.product = pre;
   ep.col_gap = (int)pre_ld;
   ep.ld_product = 2 * pre_ld;
   ep.stream_product = camera::product_streams(n, 2 * pre_ld);
-  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, X, ldx, d_model, d_ff, 1, W_gate, W_up, 0, (int)tiles.tiles, t, ep),
+  CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, X, ldx, d_model, d_ff, 1, W_gate, W_up, 0, (int)plan.m_tiles, t, ep),
              "gated projections launch");
   return CAMERA_OK;
 }
 // out[e][r][c] = left row e * rows + r times column c of the right matrix, whose d_model columns are given as rows: [d_model][k].
+// part_rows: room for group_parts_bytes of them.
 int gated_product(camera_ctx* ctx, hipStream_t stream, int dtype, int groups, int64_t rows, int64_t k, const void* left, const void* right,
-                  int64_t d_model, void* out, int64_t ld_out, int64_t expert_gap) {
+                  int64_t d_model, void* out, int64_t ld_out, int64_t expert_gap, float* part_rows) {
   const int64_t half = d_model / 2;
-  const camera::GroupTiles tiles = camera::group_tiles(dtype, groups, rows, half);
+  const camera::GroupPlan plan = camera::group_plan(dtype == CAMERA_BF16, groups, rows, half, k, camera::kMostParts);
   camera::BucketTables t{};
   t.zeros = ctx->zeros;
   camera::GemmEpilogue ep;
-  ep.mode = camera::GemmEpilogue::kRounded;
+  ep.mode = plan.parts > 1 ? camera::GemmEpilogue::kPart : camera::GemmEpilogue::kRounded;
   ep.group_rows = (int)rows;
-  ep.small_tiles = tiles.small;
-  ep.rounded = out;
-  ep.ld_product = ld_out;
+  ep.small_tiles = plan.small;
   ep.col_gap = (int)half;
-  ep.expert_gap = expert_gap;
+  if (plan.parts > 1) {
+    ep.product = part_rows;
+    ep.ld_product = d_model;
+    ep.part_stride = groups * rows * d_model;
+    ep.split_plan = {plan.parts, plan.blocks};
+  } else {
+    ep.rounded = out;
+    ep.ld_product = ld_out;
+    ep.expert_gap = expert_gap;
+  }
   const size_t es = dtype == CAMERA_BF16 ? 2 : 4;
   CAMERA_HIP(camera::launch_grouped_gemm(stream, dtype, left, k, k, half, groups, right, static_cast<const char*>(right) + es * half * k, 0,
-                                         (int)tiles.tiles, t, ep),
+                                         (int)plan.m_tiles, t, ep),
              "gated product launch");
+  if (plan.parts > 1)
+    CAMERA_HIP(camera::launch_sum_parts(stream, dtype, part_rows, plan.parts, ep.part_stride, groups, rows, d_model, out, ld_out, expert_gap),
+               "sum of parts launch");
   return CAMERA_OK;
 }
 }  // namespace
@@ -1327,6 +1339,7 @@ int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int
   const size_t o_wt = cv.take(dX != nullptr ? es * d_model * 2 * f_pad : 0);
   const size_t o_cols = cv.take(weights ? es * 2 * d_ff * n_pad : 0);
   const size_t o_xt = cv.take(weights ? es * d_model * n_pad : 0);
+  const size_t o_parts = cv.take(camera::group_parts_bytes((int64_t)sizeof(float) * d_model * std::max(dX != nullptr ? n : 0, weights ? 2 * d_ff : 0)));
   DeviceGuard guard;
   CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
   hipStream_t stream = static_cast<hipStream_t>(stream_);
@@ -1337,6 +1350,7 @@ int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int
   }
   if (int rc = ensure_workspace(ctx, cv.used)) return rc;
   char* ws = static_cast<char*>(ctx->ws);
+  float* part_rows = reinterpret_cast<float*>(ws + o_parts);
   if (pre == nullptr) {
     float* made = reinterpret_cast<float*>(ws + o_pre);
     if (int rc = gated_projections(ctx, stream, X, dtype, n, d_model, ldx, W_gate, W_up, d_ff, nullptr, 0, made)) return rc;
@@ -1351,14 +1365,14 @@ int camera_gated_ffn_backward(camera_ctx* ctx, void* stream_, const void* X, int
   }
   Bracket b(ctx, stream, CAMERA_K_GEMM);
   if (dX != nullptr)  // [dG | dU] times [W_gate; W_up]
-    if (int rc = gated_product(ctx, stream, dtype, 1, n, 2 * f_pad, ws + o_rows, ws + o_wt, d_model, dX, lddx, 0)) return rc;
+    if (int rc = gated_product(ctx, stream, dtype, 1, n, 2 * f_pad, ws + o_rows, ws + o_wt, d_model, dX, lddx, 0, part_rows)) return rc;
   if (weights) {  // two groups of left rows, dG^T and dU^T, or one of them
     const bool both = dW_gate != nullptr && dW_up != nullptr;
     const char* left = ws + o_cols + (dW_gate == nullptr ? es * d_ff * n_pad : 0);
     // group 1 continues behind group 0's rows: bring it to its own matrix
     const int64_t gap = !both ? 0 : (reinterpret_cast<intptr_t>(dW_up) - reinterpret_cast<intptr_t>(dW_gate)) / (int64_t)es - d_ff * d_model;
     if (int rc = gated_product(ctx, stream, dtype, both ? 2 : 1, d_ff, n_pad, left, ws + o_xt, d_model, dW_gate != nullptr ? dW_gate : dW_up,
-                               d_model, gap))
+                               d_model, gap, part_rows))
       return rc;
   }
   return CAMERA_OK;

@@ -69,8 +69,9 @@ int gemm_tile_m(int dtype, int64_t d_ff);
 //   kGated   silu(G) U goes to hidden[slot][ld_hidden] in the inputs' type (if hidden), G and U to product as above (if product),
 //            X indexed by token; columns d_ff .. the next multiple of 8 (bf16) or 4 are written too, zeros in hidden
 //   kRounded kProduct in the inputs' type: rounded[slot * ld_product + e * expert_gap + c], and c + col_gap
+//   kPart    kProduct, the K extent in split_plan.most_parts parts (split_plan.blocks workgroups) as GroupPlan has them
 struct GemmEpilogue {
-  enum Mode { kStats = 0, kHidden = 1, kProduct = 2, kGated = 3, kRounded = 4 };
+  enum Mode { kStats = 0, kHidden = 1, kProduct = 2, kGated = 3, kRounded = 4, kPart = 5 };
   int mode = kStats;
   float* part_phi2 = nullptr;
   float* part_max = nullptr;
@@ -89,19 +90,11 @@ struct GemmEpilogue {
   int64_t ld_hidden = 0;
   void* rounded = nullptr;
   int64_t expert_gap = 0;
-  // kGated, kRounded: n_experts groups of group_rows left rows, one behind the other, cut as group_tiles says; of the bucket
-  // tables only `zeros` is read
+  // kGated, kRounded, kPart: n_experts groups of group_rows left rows, one behind the other, cut as a GroupPlan says; of the
+  // bucket tables only `zeros` is read
   int group_rows = 0;
   bool small_tiles = false;
 };
-// How the left rows of those two are cut: tile height, tiles in all (max_tiles of the launch), and whether in small tiles.
-struct GroupTiles {
-  int tile_m = 0;
-  bool small = false;
-  int64_t tiles = 0;
-};
-constexpr int kSmallTilesBelow = 256;
-GroupTiles group_tiles(int dtype, int groups, int64_t rows, int64_t d_ff);
 hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int64_t ldx, int64_t d_model,
                                int64_t d_ff, int n_experts, const void* W_gate, const void* W_up,
                                int64_t stride_gu, int max_tiles, const BucketTables& t, const GemmEpilogue& ep);
@@ -338,10 +331,18 @@ struct GatedOperands {
   void *rows, *cols, *w_t, *x_t;
 };
 hipError_t launch_gated_operands(hipStream_t stream, int dtype, const GatedOperands& a);
+// out[e * expert_gap + r * ld + c] = the sum over the parts of part[p][r][c], in their order, in `dtype`; r of all groups of
+// group_rows rows, e the group of r; cols a multiple of 4.
+hipError_t launch_sum_parts(hipStream_t stream, int dtype, const float* part, int parts, int64_t part_stride, int groups, int64_t group_rows,
+                            int64_t cols, void* out, int64_t ld, int64_t expert_gap);
 // vectors of 16 bytes set to zero
 hipError_t launch_zero(hipStream_t stream, void* dst, int64_t vectors);
 // H and / or pre of up to kGatedRowsMost tokens, bf16: every weight row is read once, straight into matrix operands.
 constexpr int kGatedRowsMost = 64;
+// Where that beats tiles: up to one tile of tokens always, beyond it while there is at most one workgroup of 16 channels a compute unit
+// (each reads every token again).  us, by rows / in tiles: 2560 x 3584, 64 tokens 24 / 36; 14336 x 4096, 16 tokens 48 / 47, 32
+// tokens 62 / 47, 64 tokens 99 / 47.
+inline bool gated_by_rows(int64_t n, int64_t d_ff) { return n <= 16 || (n <= kGatedRowsMost && d_ff <= 16 * 256); }
 hipError_t launch_gated_rows(hipStream_t stream, const void* X, int64_t ldx, int64_t n, int64_t d_model, const void* W_gate,
                              const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre, int64_t pre_ld);
 

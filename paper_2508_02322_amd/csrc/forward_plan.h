@@ -124,6 +124,53 @@ inline int64_t compact_product_workspace(int64_t pairs, int64_t experts, bool ti
   return std::max(product_workspace(pairs * row_bytes, k_ext), chunks * (kStreamingTokens * experts - 1) * row_bytes);
 }
 
+// ---- products of plain groups of rows (the gated block and its gradients) ------------------------------------------------
+// bf16: tiles of 256 x 128 x 2, one workgroup a compute unit, or where they are few small ones of 64 x 64 x 2, up to three a
+// unit; float32: 64 x 32 x 2, up to six.
+constexpr int kPlanSmallM = 64, kPlanSmallN = 64, kPlanF32M = 64, kPlanF32N = 32, kPlanF32K = 32;
+struct GroupPlan {
+  bool small = false;
+  int parts = 1;         // of K
+  int64_t m_tiles = 0;   // of all groups
+  int64_t blocks = 0;    // workgroups of a launch in parts
+};
+// Time in ns of `here` workgroups on every die with k K tiles each: full-sized tiles in rounds as in split_ns; small ones, all at
+// once, by how many a unit has: 0.56, 0.69 and 0.82 us per K tile with one, two and three.  (More than that many small tiles draw the
+// chip's whole power and are slower than full-sized ones: dW of 8192 tokens, 2560 x 3584, 430 us in 2240 small tiles, 330 in 280.)
+inline int64_t group_ns(bool small, int64_t here, int64_t k) {
+  const int64_t die_cus = kPlanCus / kPlanDies, on_unit = (here + die_cus - 1) / die_cus;
+  if (!small) return on_unit * (1400 * k + 8000);
+  return on_unit > 3 ? INT64_MAX : (430 + 130 * on_unit) * k + 6000;
+}
+// most_parts: 1 where a product cannot be taken in parts.  A part's float32 rows (product_bytes) are written and read again at
+// 6 TB/s, in a launch more; they stay within the memory-side cache.
+inline GroupPlan group_plan(bool bf16, int64_t groups, int64_t rows, int64_t half_columns, int64_t k_ext, int most_parts) {
+  auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  const int64_t product_bytes = groups * rows * 2 * half_columns * 4;
+  GroupPlan best, best_parts;
+  int64_t best_ns = -1, best_parts_ns = -1;
+  for (int small = 0; small < (bf16 ? 2 : 1); ++small) {
+    const int64_t m = bf16 ? (small ? kPlanSmallM : kPlanTileM) : kPlanF32M, n = bf16 ? (small ? kPlanSmallN : kPlanTileN) : kPlanF32N;
+    const int64_t m_tiles = groups * up(rows, m), tiles = m_tiles * up(half_columns, n), k_tiles = up(k_ext, bf16 ? kPlanTileK : kPlanF32K);
+    for (int p = 1; p <= most_parts; ++p) {
+      if (p > 1 && (k_tiles < 8 * p || p * product_bytes > kPlanCacheBytes)) break;
+      // float32: a unit's workgroups share its matrix pipe, 0.6 us per K tile each, and fewer than three wait 1.4 us for theirs
+      const int64_t here = tiles_per_die(tiles) * p;
+      int64_t ns = bf16 ? group_ns(small, here, up(k_tiles, p)) : up(k_tiles, p) * std::max<int64_t>(1400, 600 * up(here, kPlanCus / kPlanDies)) + 5000;
+      if (ns == INT64_MAX) break;
+      if (p > 1) ns += p * 2 * product_bytes / 6000 + 4000;
+      int64_t& least = p > 1 ? best_parts_ns : best_ns;
+      if (least < 0 || ns < least) {
+        least = ns;
+        (p > 1 ? best_parts : best) = {small != 0, p, m_tiles, tiles_per_die(tiles) * p * kPlanDies};
+      }
+    }
+  }
+  return best_parts_ns >= 0 && split_pays(best_parts_ns, best_ns) ? best_parts : best;
+}
+// Bytes of the parts' rows that a product and every smaller one with as many columns may take.
+inline int64_t group_parts_bytes(int64_t product_bytes) { return std::min(kMostParts * product_bytes, kPlanCacheBytes); }
+
 // When a masked call's first contraction is prepared to go over the list of the kept micro-experts: the list, the work table and the
 // zeros are three launches before it (12-16 us where the list is not used, the zeros on top where it is), and a launch with few
 // more tiles than compute units gains little from fewer.  Below the line a list won 4 us of 124 (2.5e10 products, 40 % pruned) or lost.

@@ -149,6 +149,25 @@ __global__ __launch_bounds__(kThreads) void gated_operands_kernel(GatedOperands 
                       id / across_n * kTile, cells);
 }
 
+// Four columns a thread, a row (of all groups) or more a workgroup.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sum_parts_kernel(const float* __restrict__ part, int parts, int64_t part_stride, int64_t rows,
+                                                             int64_t group_rows, int64_t cols, T* __restrict__ out, int64_t ld,
+                                                             int64_t expert_gap) {
+  const int64_t quads = cols / 4;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * quads; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = i / quads, c = (i - row * quads) * 4;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(part + row * cols + c);
+    for (int p = 1; p < parts; ++p) sum += *reinterpret_cast<const f32x4*>(part + p * part_stride + row * cols + c);
+    struct alignas(4 * sizeof(T)) Quad {
+      T v[4];
+    } q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q.v[j] = (T)sum[j];
+    *reinterpret_cast<Quad*>(out + row / group_rows * expert_gap + row * ld + c) = q;
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void zero_kernel(uint4* __restrict__ dst, int64_t vectors) {
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) dst[i] = uint4{0, 0, 0, 0};
 }
@@ -237,6 +256,20 @@ hipError_t launch_gated_operands(hipStream_t stream, int dtype, const GatedOpera
   if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   if (dtype == CAMERA_BF16) hipLaunchKernelGGL((gated_operands_kernel<__bf16>), launch_grid(blocks), dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((gated_operands_kernel<float>), launch_grid(blocks), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_sum_parts(hipStream_t stream, int dtype, const float* part, int parts, int64_t part_stride, int groups, int64_t group_rows,
+                            int64_t cols, void* out, int64_t ld, int64_t expert_gap) {
+  const int64_t rows = groups * group_rows;
+  const int64_t blocks = std::min<int64_t>((rows * (cols / 4) + kThreads - 1) / kThreads, 8192);
+  if (blocks < 1 || cols % 4 != 0) return hipErrorInvalidValue;
+  if (dtype == CAMERA_BF16)
+    hipLaunchKernelGGL((sum_parts_kernel<__bf16>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, part, parts, part_stride, rows,
+                       group_rows, cols, static_cast<__bf16*>(out), ld, expert_gap);
+  else
+    hipLaunchKernelGGL((sum_parts_kernel<float>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, part, parts, part_stride, rows,
+                       group_rows, cols, static_cast<float*>(out), ld, expert_gap);
   return hipGetLastError();
 }
 

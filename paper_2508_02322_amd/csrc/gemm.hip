@@ -105,11 +105,13 @@ constexpr int kChunkM = 4;     // otherwise this many
 //   kEpiGated   : silu(gate) * up in the inputs' type -> hidden (if there is one) and gate and up themselves, float32 -> product
 //                 [row][column] and [column + col_gap] (if there is one); columns up to the next multiple of pad_hidden are written too
 //   kEpiRounded : kEpiProduct in the inputs' type -> rounded, the rows of expert e expert_gap elements further on for each e
-enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3, kEpiGated = 4, kEpiRounded = 5 };
+//   kEpiPart    : kEpiProduct, the K extent in ep.k_parts parts
+enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3, kEpiGated = 4, kEpiRounded = 5, kEpiPart = 6 };
 constexpr bool epi_hidden(int epi) { return epi == kEpiHidden || epi == kEpiListed; }
-constexpr bool epi_by_slot(int epi) { return epi == kEpiProduct || epi == kEpiRounded; }  // token rows = bucket slots
-// These two have groups of ep.group_rows left rows each, one behind the other, and no bucket tables.
-constexpr bool epi_plain(int epi) { return epi == kEpiGated || epi == kEpiRounded; }
+constexpr bool epi_by_slot(int epi) { return epi == kEpiProduct || epi == kEpiRounded || epi == kEpiPart; }  // token rows = bucket slots
+constexpr bool epi_product(int epi) { return epi == kEpiProduct || epi == kEpiPart; }  // float32 product rows, K in parts
+// These three have groups of ep.group_rows left rows each, one behind the other, and no bucket tables.
+constexpr bool epi_plain(int epi) { return epi == kEpiGated || epi == kEpiRounded || epi == kEpiPart; }
 struct EpiArgs {
   float* part_phi2;
   float* part_max;
@@ -129,7 +131,7 @@ struct EpiArgs {
   int64_t blocks;          // workgroups, where not every token tile there may be has one for every part (host)
   void* rounded;           // kEpiRounded: row stride ld_product
   int64_t expert_gap;
-  int group_rows;          // kEpiGated, kEpiRounded
+  int group_rows;          // kEpiGated, kEpiRounded, kEpiPart
 };
 
 // One wave instruction of the direct global -> LDS path: lane l's 16 bytes at p (+ IMM) go to LDS bytes
@@ -586,7 +588,7 @@ __device__ __forceinline__ void tile_body16(const TileState<C>& st, int n0, int 
   // Epilogue.  Accumulator register r of lane l in sub-block (a, b) of block (i, j) is output row
   // 32*block + 16a + 4*(l/16) + r, channel tile_channel(32*j + 16b + l % 16) of the wave's.
   const int lane_col = st.frag_row, lane_rows = st.frag_half * 4;  // l % 16, 4 * (l / 16)
-  if constexpr (EPI == kEpiProduct) {
+  if constexpr (epi_product(EPI)) {
     static_assert(TN == 2, "a lane's channels of the four sub-blocks are consecutive");
     const int col0 = n0 + st.wave_n * TN * 32 + 4 * lane_col;  // this lane's four channels
     auto write = [&](auto stream) {
@@ -973,7 +975,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void grouped_gemm_bf
   int seq = block / kXcds;
   const int first = (block % kXcds) * per_xcd;
   [[maybe_unused]] int part = 0, parts = 1;
-  if constexpr (EPI == kEpiProduct) {  // the tiles of an XCD with the first part of K, then with the second, ...
+  if constexpr (epi_product(EPI)) {  // the tiles of an XCD with the first part of K, then with the second, ...
     const int here = max(0, min(per_xcd, total - first));
     parts = ep.k_parts;
     if (ep.parts != nullptr) {
@@ -1017,7 +1019,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerSimd) void grouped_gemm_bf
   w.n0 = n0;
   w.tok_first = tile_in_expert * BM;
   constexpr int kAux = C::kAliasAux ? 0 : C::kRingBytes;  // the per-tile arrays
-  if constexpr (EPI == kEpiProduct) {
+  if constexpr (epi_product(EPI)) {
     const KPart k = k_part<C>(d_model, part, parts);
     ep.product += part * ep.part_stride;
     run_tile<C, TAIL, EPI, kAux>(w, X + k.begin, ldx, k.length, d_ff, Wg + k.begin, Wu + k.begin, stride_gu, d_model, perm, w_perm,
@@ -1333,7 +1335,17 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
   const int total = first_tile(n_experts) * n_tiles_n;
   const int per_xcd = (total + kXcds - 1) / kXcds;
   const int block = linear_block();
-  const int seq = block / kXcds;
+  int seq = block / kXcds;
+  [[maybe_unused]] int k_begin = 0, k_end = d_model;
+  if constexpr (EPI == kEpiPart) {  // as in the bf16 kernel
+    const int here = max(0, min(per_xcd, total - (block % kXcds) * per_xcd));
+    if (seq >= here * ep.k_parts) return;
+    const int part = seq / here, k_tiles = (d_model + F32_KT - 1) / F32_KT;
+    seq -= part * here;
+    k_begin = k_tiles * part / ep.k_parts * F32_KT;
+    k_end = min(d_model, k_tiles * (part + 1) / ep.k_parts * F32_KT);
+    ep.product += part * ep.part_stride;
+  }
   const int logical = (block % kXcds) * per_xcd + seq;
   if (seq >= per_xcd || logical >= total) return;
   int e;
@@ -1391,8 +1403,9 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
   const float* fg = &s_w[0][(wave_n * 16 + col) * kF32Row + quarter * 4];
   const float* fu = &s_w[1][(wave_n * 16 + col) * kF32Row + quarter * 4];
   const bool active = wave_m * 32 < m_len;  // wave-uniform: a wave without tokens only brings in its share of the tiles
-  fetch(0);
-  for (int k0 = 0; k0 < d_model; k0 += F32_KT) {
+  const int k_from = EPI == kEpiPart ? k_begin : 0, k_to = EPI == kEpiPart ? k_end : d_model;
+  fetch(k_from);
+  for (int k0 = k_from; k0 < k_to; k0 += F32_KT) {
     __syncthreads();  // the previous tile has been read
     const bool k_ok = k0 + lk < d_model;
     const f32x4 zero = {};
@@ -1432,7 +1445,7 @@ __global__ __launch_bounds__(256, 6) void grouped_gemm_f32_kernel(
     for (int i = 0; i < 4; ++i) {
       const int row = wave_m * 32 + b * 16 + quarter * 4 + i;
       const int64_t out_row = row_first + row;
-      if constexpr (EPI == kEpiProduct) {
+      if constexpr (epi_product(EPI)) {
         if (row < m_len && c < d_ff) {
           ep.product[out_row * ep.ld_product + c] = acc_g[b][i];
           ep.product[out_row * ep.ld_product + c + ep.col_gap] = acc_u[b][i];
@@ -1571,17 +1584,7 @@ bool fits_32bit_offsets(int64_t a_rows, int64_t lda, int64_t b_rows, int64_t ldw
 
 }  // namespace
 
-GroupTiles group_tiles(int dtype, int groups, int64_t rows, int64_t d_ff) {
-  GroupTiles g;
-  g.tile_m = dtype == CAMERA_BF16 ? Bf16Cfg::BM : F32_BM;
-  const int64_t columns = (d_ff + Bf16Cfg::BN - 1) / Bf16Cfg::BN;
-  if (dtype == CAMERA_BF16 && groups * ((rows + Bf16Cfg::BM - 1) / Bf16Cfg::BM) * columns < kSmallTilesBelow) {
-    g.small = true;
-    g.tile_m = SmallCfg::BM;
-  }
-  g.tiles = groups * ((rows + g.tile_m - 1) / g.tile_m);
-  return g;
-}
+static_assert(SmallCfg::BM == kPlanSmallM && SmallCfg::BN == kPlanSmallN && F32_BM == kPlanF32M && F32_BN == kPlanF32N && F32_KT == kPlanF32K, "the plan's tiles");
 
 int gemm_tile_m(int dtype, int64_t d_ff) {
   (void)d_ff;
@@ -1641,18 +1644,23 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
       case GemmEpilogue::kRounded:
         return (e.small_tiles ? launch_bf16<kEpiRounded, SmallCfg> : launch_bf16<kEpiRounded>)(stream, X, ldx, d_model, d_ff, n_experts,
                                                                                                W_gate, W_up, stride_gu, max_tiles, t, ep);
+      case GemmEpilogue::kPart:
+        return (e.small_tiles ? launch_bf16<kEpiPart, SmallCfg> : launch_bf16<kEpiPart>)(stream, X, ldx, d_model, d_ff, n_experts, W_gate,
+                                                                                         W_up, stride_gu, max_tiles, t, ep);
       default:
         return hipErrorInvalidValue;
     }
   }
-  const int64_t n_blocks = (max_tiles * ((d_ff + F32_BN - 1) / F32_BN) + kXcds - 1) / kXcds * kXcds;
+  int64_t n_blocks = (max_tiles * ((d_ff + F32_BN - 1) / F32_BN) + kXcds - 1) / kXcds * kXcds;
+  if (e.mode == GemmEpilogue::kPart) n_blocks = ep.blocks;
   if (n_blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   auto kern = e.mode == GemmEpilogue::kStats    ? grouped_gemm_f32_kernel<kEpiStats>
               : e.mode == GemmEpilogue::kHidden ? grouped_gemm_f32_kernel<kEpiHidden>
               : e.mode == GemmEpilogue::kGated  ? grouped_gemm_f32_kernel<kEpiGated>
               : e.mode == GemmEpilogue::kRounded ? grouped_gemm_f32_kernel<kEpiRounded>
+              : e.mode == GemmEpilogue::kPart    ? grouped_gemm_f32_kernel<kEpiPart>
                                                 : grouped_gemm_f32_kernel<kEpiProduct>;
-  if (e.mode < GemmEpilogue::kStats || e.mode > GemmEpilogue::kRounded) return hipErrorInvalidValue;
+  if (e.mode < GemmEpilogue::kStats || e.mode > GemmEpilogue::kPart) return hipErrorInvalidValue;
   hipLaunchKernelGGL(kern, launch_grid(n_blocks), dim3(256), 0, stream, static_cast<const float*>(X), ldx, (int)d_model,
                      (int)d_ff, static_cast<const float*>(W_gate), static_cast<const float*>(W_up), stride_gu, t.offsets,
                      t.tile_offset, t.tile_expert, t.perm, t.w_perm, n_experts, ep);
