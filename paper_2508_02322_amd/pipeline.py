@@ -12,6 +12,9 @@ the tensors of ``inputs.make_layer`` (``X, W_r, bias, W_gate, W_up, W_down`` and
                 experts' matrices reordered by precision class, row-wise for W_up / W_gate (CAMERA-Q: a micro-expert
                 keeps one precision) or column-wise (the comparison variant CAMERA-Q-dagger: every matrix sliced along
                 its input dimension)
+  teacher_of, recovery_step   repairing a pruned model: what the original model says at every position, and the pruned model's
+                log probabilities, its distance from the original and the gradient of both with respect to its logits
+  CompactLayer.block, .block_backward   the gated block of one expert of the pruned layer and its gradients
 """
 from __future__ import annotations
 
@@ -71,6 +74,24 @@ class CompactLayer:
         """The pruned layer's output for tokens X with routing (topk_idx, topk_w)."""
         return cam.layer_forward_compact(X, topk_idx, topk_w, self.counts, self.W_gate, self.W_up, self.W_down,
                                          n_shared=self.n_shared, down_row_align=self.row_align, Y=Y, accumulate=accumulate)
+
+    def expert(self, e: int):
+        """(W_gate [count, d_model], W_up [count, d_model], W_down [d_model, count]) of expert e: views of the packed matrices."""
+        at, d = sum(self.counts[:e]), self.W_gate.shape[1]
+        ld = [-(-c // self.row_align) * self.row_align for c in self.counts[:e + 1]]
+        start, count = d * sum(ld[:e]), self.counts[e]
+        down = self.W_down[start:start + d * ld[e]].view(d, ld[e])[:, :count]
+        return self.W_gate[at:at + count], self.W_up[at:at + count], down
+
+    def block(self, cam, e: int, X, want_pre: bool = False):
+        """silu(X W_gate^T) * (X W_up^T) of the micro-experts that expert e kept (at least one)."""
+        W_gate, W_up, _ = self.expert(e)
+        return cam.gated_ffn(X, W_gate, W_up, want_pre=want_pre)
+
+    def block_backward(self, cam, e: int, X, dH, pre=None):
+        """(dX, dW_gate, dW_up) of that block."""
+        W_gate, W_up, _ = self.expert(e)
+        return cam.gated_ffn_backward(X, W_gate, W_up, dH, pre=pre)
 
 
 def prune_layer(cam, layer: dict, scores: LayerScores, ratio: float, row_align: int = 64) -> CompactLayer:
@@ -138,3 +159,37 @@ def cameraq_dagger_layer(cam, layer: dict, scores: LayerScores, bits, ratios) ->
     _, _, gate = cam.gather_micro_experts(None, None, Wg, perm_in)
     _, _, up = cam.gather_micro_experts(None, None, Wu, perm_in)
     return MixedPrecisionLayer(bits_down, count_down, down, bits_in, count_in, gate, up, True)
+
+
+@dataclasses.dataclass
+class Teacher:
+    """The original model's most likely tokens at every position."""
+    idx: torch.Tensor           # int32 [n, k]: -1 where a masked position has fewer
+    logprob: torch.Tensor       # float32 [n, k], at `temperature`
+    temperature: float
+
+
+def teacher_of(cam, logits, top_k: int, temperature: float = 1.0) -> Teacher:
+    out = cam.token_logprobs(logits, top_k=top_k, temperature=temperature)
+    return Teacher(out["top_idx"], out["top_logprob"], temperature)
+
+
+@dataclasses.dataclass
+class RecoveryStep:
+    logprob: torch.Tensor       # float32 [n]: of the targets, 0 where a position has none
+    entropy: torch.Tensor       # float32 [n]
+    kl: torch.Tensor            # float32 [n]: distance from the teacher
+    dlogits: torch.Tensor       # [n, vocab], the logits' type
+
+
+def recovery_step(cam, logits, targets, teacher: Teacher, grad_logprob, grad_kl, tail: bool = True, dlogits=None) -> RecoveryStep:
+    """One step of repairing a pruned model: the log probabilities of the targets (at temperature 1), the divergence from the
+    teacher (at the teacher's temperature; tail: its unlisted tokens as one class), and the gradient with respect to the logits of
+    sum(grad_logprob * logprob) + sum(grad_kl * kl).  For a mean over n positions with weight w on the teacher: grad_logprob =
+    -(1 - w) / n, grad_kl = w / n (times the temperature squared, if its gradient is to keep its size)."""
+    lp = cam.token_logprobs(logits, targets)
+    kd = cam.distill_topk(logits, teacher.idx, teacher.logprob, temperature=teacher.temperature, tail=tail)
+    dlogits = cam.token_logprobs_backward(logits, targets, lp["stats"], grad_logprob, dlogits=dlogits)
+    cam.distill_topk_backward(logits, teacher.idx, teacher.logprob, kd["stats"], grad_kl, temperature=teacher.temperature, tail=tail,
+                              dlogits=dlogits, accumulate=True)
+    return RecoveryStep(lp["logprob"], lp["entropy"], kd["loss"], dlogits)

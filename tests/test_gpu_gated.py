@@ -88,6 +88,22 @@ def test_bf16_block(cam, n, d, f):
     check(cam, n, d, f, "bf16")
 
 
+# How dX is computed: tiles, and whether K is in parts.
+FORMS = {(40, 128, 5000, "bf16"): ("small", True), (700, 256, 200, "bf16"): ("small", False), (4096, 2048, 200, "bf16"): ("full", False),
+         (2048, 3584, 4000, "bf16"): ("full", True), (300, 772, 517, "f32"): ("full", True), (300, 772, 40, "f32"): ("full", False)}
+
+
+@pytest.mark.parametrize("n,d,f,dtype", list(FORMS))
+def test_every_form(cam, n, d, f, dtype):
+    check(cam, n, d, f, dtype)
+
+
+@pytest.mark.parametrize("n,d,f", [(3, 128, 4100), (17, 128, 4100), (64, 72, 4096), (16, 40, 9), (1, 8200, 40)])
+def test_bf16_few_tokens(cam, n, d, f):
+    """By rows and in tiles, on both sides of where they meet."""
+    check(cam, n, d, f, "bf16")
+
+
 @pytest.mark.parametrize("n,d,f", [(1, 4, 1), (3, 12, 5), (64, 32, 32), (65, 260, 33), (300, 772, 517)])
 def test_f32_block(cam, n, d, f):
     check(cam, n, d, f, "f32")

@@ -1,0 +1,170 @@
+"""The calls that judge and repair a pruned model, as they are used together: the original model's alternatives, the pruned model's
+log probabilities and its distance, their gradient with respect to the logits, and from there through the packed layer's gated block.
+
+Tolerances.  float32 results as in the tests of the single calls.  In the gradient two bf16 roundings meet (the first call's
+result, and its sum with the second's), each half a step, 2^-8 relative to the value it rounds: no larger than the two gradients'
+magnitudes together.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2508_02322_amd import inputs, pipeline
+from tests import helpers as H
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = 2.0 ** -8
+
+
+def pruned_layer(cam, ratio=0.4, seed_cfg="deepseek-moe-16b"):
+    cfg = inputs.scaled(inputs.CONFIGS[seed_cfg], n_tokens=300, d_model=128, d_ff=200, n_experts=4, top_k=2, n_shared=1, d_ff_shared=264,
+                        n_layers=1, energy_spread=0.5)
+    layer = H.to_dev(inputs.make_layer(cfg, 0, device="cpu"))
+    scores = pipeline.score_layer(cam, layer, cfg.top_k, cfg.alpha)
+    return layer, scores, pipeline.prune_layer(cam, layer, scores, ratio)
+
+
+def test_expert_views_are_the_kept_rows(cam):
+    layer, scores, pruned = pruned_layer(cam)
+    kept = pruned.kept_idx.cpu()
+    for e in range(5):
+        name, lo, hi = ("W", scores.seg_offsets[e], scores.seg_offsets[e + 1])
+        rows = kept[(kept >= lo) & (kept < hi)].long() - lo
+        src = [layer[k][e] for k in ("W_gate", "W_up", "W_down")] if e < 4 else [layer[k][0] for k in ("Ws_gate", "Ws_up", "Ws_down")]
+        gate, up, down = pruned.expert(e)
+        assert torch.equal(gate, src[0][rows.cuda()]) and torch.equal(up, src[1][rows.cuda()]) and torch.equal(down, src[2][:, rows.cuda()])
+
+
+def test_block_of_the_shared_expert_is_the_layer(cam):
+    """The block of the shared expert times its W_down is what the packed layer adds for it."""
+    layer, scores, pruned = pruned_layer(cam)
+    X = layer["X"]
+    e = 4
+    W_down = pruned.expert(e)[2]
+    only = pipeline.CompactLayer([pruned.counts[e]], 0, pruned.row_align, *pruned.expert(e)[:2],
+                                 pruned.W_down[-128 * (-(-pruned.counts[e] // 64) * 64):], None, None)
+    want = only.forward(cam, X, None, None)
+    got = pruned.block(cam, e, X).float() @ W_down.float().t()
+    # the same bf16 hidden values but for sums in another order: a flipped rounding, 2^-7 of a value, now and then
+    scale = (pruned.block(cam, e, X).float().abs() @ W_down.float().abs().t())
+    assert float(((got - want).abs() / scale).max()) < 2.0 ** -7
+
+
+def step64(logits, targets, teacher, g_lp, g_kl, T):
+    """Per-row log probability and divergence, and the gradient, by autograd in float64 from the definitions."""
+    z = logits.double().detach().requires_grad_(True)
+    n, vocab = z.shape
+    lp = torch.log_softmax(z, 1)
+    has = targets >= 0
+    logprob = torch.where(has, lp[torch.arange(n, device="cuda"), targets.long().clamp(min=0)], 0.0)
+    lpT = torch.log_softmax(z / T, 1)
+    t = teacher.logprob.double()
+    q = t.exp()
+    listed = lpT.gather(1, teacher.idx.long())
+    marks = torch.zeros(n, vocab, dtype=torch.bool, device="cuda").scatter_(1, teacher.idx.long(), True)
+    rest = torch.logsumexp(lpT.masked_fill(marks, -math.inf), 1)
+    left = 1 - q.sum(1)
+    kl = (q * (t - listed)).sum(1) + left * (left.log() - rest)
+    a, = torch.autograd.grad((g_lp.double() * logprob).sum(), z, retain_graph=True)
+    b, = torch.autograd.grad((g_kl.double() * kl).sum(), z)
+    return logprob.detach(), kl.detach(), a, b
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_recovery_step(cam, dtype):
+    n, vocab, T = 37, 5003, 2.0
+    g = torch.Generator(device="cuda").manual_seed(1)
+    original = (3 * torch.randn((n, vocab), generator=g, device="cuda")).to(dtype)
+    logits = (original.float() + 0.5 * torch.randn((n, vocab), generator=g, device="cuda")).to(dtype)
+    targets = original.float().argmax(1).int()
+    targets[::5] = -100
+    teacher = pipeline.teacher_of(cam, original, 24, T)
+    g_lp = torch.full((n,), -0.5 / n, device="cuda")
+    g_kl = torch.full((n,), 0.5 * T * T / n, device="cuda")
+    out = pipeline.recovery_step(cam, logits, targets, teacher, g_lp, g_kl)
+    torch.cuda.synchronize()
+    logprob, kl, a, b = step64(logits, targets, teacher, g_lp, g_kl, T)
+    L = vocab / 512 + 40
+    assert float((out.logprob.double() - logprob).abs().max()) < (4 * float(logprob.abs().max()) + L + 8) * U
+    assert float((out.kl.double() - kl).abs().max()) < (8 * 30 + 2 * L + 16) * U
+    half = HALF if dtype == torch.bfloat16 else U
+    err = (out.dlogits.double() - a - b).abs()
+    # An unlisted token's gradient is p (mass - q_r / p_r) g / T with p at temperature T.  q_r / p_r, about 1 here as mass is, carries
+    # the row's sums (2 L u) and log probabilities of up to 30 (4 x 30 u), so the bracket is off by 2 (2 L + 120 + 16) u at most,
+    # however much of it cancels.
+    bracket = 2 * (2 * L + 4 * 30 + 16) * U
+    p_T = (logits.double() / T).softmax(1)
+    tol = (half + 64 * 4 * U) * 2 * (a.abs() + b.abs()) + bracket * g_kl.double()[:, None] / T * p_T + 2.0 ** -126
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+def test_recovery_through_the_block(cam):
+    """Logits = (block of the pruned shared expert) W_down^T W_head^T; the gradients of the kept rows and of the tokens against autograd
+    in float64.  dH reaches the block in bf16 (half a step), the block rounds dG, dU and its results: with independent
+    errors of at most 2^-8 each, four of them are within 2 x 2^-8 in the 2-norm."""
+    layer, scores, pruned = pruned_layer(cam)
+    X, e, vocab = layer["X"], 4, 1003
+    n = X.shape[0]
+    gate, up, down = pruned.expert(e)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    head = torch.randn((vocab, 128), generator=gen, device="cuda") * 4.0
+    to_logits = (head @ down.float()).t().contiguous()           # [count, vocab]
+    original = (2 * torch.randn((n, vocab), generator=gen, device="cuda"))
+    targets = original.argmax(1).int()
+    teacher = pipeline.teacher_of(cam, original, 16)
+    g_lp, g_kl = torch.full((n,), -0.5 / n, device="cuda"), torch.full((n,), 0.5 / n, device="cuda")
+
+    Hid, pre = pruned.block(cam, e, X, want_pre=True)
+    logits = Hid.float() @ to_logits
+    step = pipeline.recovery_step(cam, logits, targets, teacher, g_lp, g_kl)
+    dH = (step.dlogits @ to_logits.t()).to(torch.bfloat16)
+    got = pruned.block_backward(cam, e, X, dH, pre=pre)
+    torch.cuda.synchronize()
+
+    x, wg, wu = (t.double().detach().requires_grad_(True) for t in (X, gate, up))
+    G, Up = x @ wg.t(), x @ wu.t()
+    h = G * torch.sigmoid(G) * Up
+    z = (h + (Hid.double() - h).detach()) @ to_logits.double()   # at the rounded hidden values that the logits were made from
+    _, _, a, b = step64(z, targets, teacher, g_lp, g_kl, 1.0)
+    want = torch.autograd.grad(z, (x, wg, wu), a + b)
+    for g, w in zip(got, want):
+        assert float((g.double() - w).norm() / w.norm()) < 2 * HALF
+
+
+def test_step_in_a_graph(cam):
+    """Block, logits, loss and gradients captured once and replayed after the inputs changed; the library's calls only."""
+    layer, scores, pruned = pruned_layer(cam)
+    X = layer["X"].clone()
+    n, vocab, e = X.shape[0], 2003, 4
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    logits = torch.randn((n, vocab), generator=gen, device="cuda").to(torch.bfloat16)
+    teacher = pipeline.teacher_of(cam, torch.randn((n, vocab), generator=gen, device="cuda").to(torch.bfloat16), 8)
+    targets = torch.randint(0, vocab, (n,), generator=gen, device="cuda").int()
+    g = torch.ones(n, device="cuda")
+    dH = torch.randn((n, pruned.counts[e]), generator=gen, device="cuda").to(torch.bfloat16)
+
+    def step():
+        Hid, pre = pruned.block(cam, e, X, want_pre=True)
+        out = pipeline.recovery_step(cam, logits, targets, teacher, g, g)
+        return (Hid, out.logprob, out.kl, out.dlogits, *pruned.block_backward(cam, e, X, dH, pre=pre))
+    step()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            captured = step()
+    for trial in range(4):
+        if trial:
+            X.copy_(torch.randn(X.shape, generator=gen, device="cuda"))
+            logits.copy_(torch.randn(logits.shape, generator=gen, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in captured]
+        for a, b in zip(kept, step()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
