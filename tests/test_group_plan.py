@@ -65,8 +65,8 @@ def test_room_for_parts_never_shrinks_with_the_batch(plan):
 
 
 def test_the_gpu_tests_reach_every_form(plan):
-    """The sizes that tests/test_gpu_gated.py names for it: small tiles, full-sized ones, either in parts."""
-    from tests.test_gpu_gated import FORMS
+    """The sizes that tests/test_gpu_repair_block.py names for it: small tiles, full-sized ones, either in parts."""
+    from tests.test_gpu_repair_block import FORMS
     for (n, d, f, dtype), form in FORMS.items():
         p = plan(dtype == "bf16", 1, n, d // 2, 2 * up(f, 64) * 64)     # dX
         assert ("small" if p["small"] else "full", p["parts"] > 1) == form, (n, d, f, p)
