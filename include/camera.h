@@ -21,7 +21,9 @@
  *     names the offending argument.  No exception or abort crosses this ABI.
  *   - The context owns a grow-only device workspace (hipMalloc on first use and
  *     on growth, which synchronises the device) and, for the ranking calls, a
- *     small persistent selection state made on their first use.
+ *     small persistent selection state made on their first use.  Growth moves
+ *     the workspace: a graph captured before it must not be replayed after it,
+ *     so make the largest call of every kind before the first capture.
  *   - NaN / Inf in the inputs: results unspecified (not checked).  (The calls on
  *     logits say what -Inf means there.)
  *   - Device data pointers must be 16-byte aligned; for CAMERA_BF16 d_model and
@@ -434,15 +436,16 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
  *   teacher_idx      int32 [n x k]; an entry outside [0, vocab) is ignored, and so is one that repeats an earlier entry of its row
  *   teacher_logprob  float32 [n x k]; an entry of -Inf is ignored.  1 <= k <= CAMERA_MAX_ALTERNATIVES.
  *   loss   float32 [n] out.  A row without entries has loss 0 (with CAMERA_DISTILL_TAIL: all of its probability is in the one
- *            class, loss 0).  +Inf where a listed token with q_j > 0 has logit -Inf.
+ *            class, loss 0).  +Inf where a listed token with q_j > 0 has logit -Inf (its gradient is what the formula gives: finite).
  *   stats  float32 [n x CAMERA_DISTILL_STATS] out, for the gradient: max of the logits, log sum exp((z - max) / temperature),
  *            log sum exp(teacher_logprob / temperature) (0 with CAMERA_DISTILL_TAIL), the sum of q, and log(q_r / p_r) (-Inf
  *            without that class): an unlisted token's part of the gradient is p (sum of q - q_r / p_r)
- * The vocabulary's sums are taken in float32, those over the listed tokens in float64.  n == 0 does nothing.
+ * The vocabulary's sums are taken in float32, those over the listed tokens in float64.  The workspace of a call serves every
+ * other, unless with CAMERA_DISTILL_TAIL vocab is above 2^18, where it grows with n.  n == 0 does nothing.
  *
  * camera_distill_topk_backward: the gradient with respect to the logits of the sum over i of grad_loss[i] loss[i]; stats, flags
  * (with CAMERA_ACCUMULATE allowed) and dlogits as above, the same teacher, temperature and CAMERA_DISTILL_TAIL as in the forward
- * call.  Rows with grad_loss 0 are set to 0 without reading their logits.
+ * call.  Rows with grad_loss 0 are set to 0 without reading their logits; so are rows whose logits are all -Inf.
  */
 int camera_distill_topk(camera_ctx* ctx, void* stream,
                         const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
@@ -473,7 +476,10 @@ int camera_distill_topk_backward(camera_ctx* ctx, void* stream,
  *   dX      [n x d_model] out, row stride lddx, a multiple of 8 (4) elements;  dW_gate, dW_up  [d_ff x d_model] out, rows
  *           contiguous; all of `dtype`.  Each may be NULL (not computed).
  * With CAMERA_BF16 dG and dU are rounded to bf16 before the products (operands of the matrix instructions), which accumulate in
- * float32 and round their result once.  n == 0 sets dW_gate and dW_up to zero.  No output may overlap an input.
+ * float32 and round their result once; where a product has few tiles its sums over K are taken in up to eight parts: how many
+ * depends on n, so the last bits may.  The workspace holds, d_ff and n rounded up to 64, 2 d_ff (n + d_model) elements for dX,
+ * n (2 d_ff + d_model) for the weight gradients, 8 n d_ff bytes without pre, and up to 256 MiB of parts: a call on the largest
+ * batch serves all smaller ones of the block.  n == 0 sets dW_gate and dW_up to zero.  No output may overlap an input.
  */
 int camera_gated_ffn(camera_ctx* ctx, void* stream,
                      const void* X, int dtype, int64_t n, int64_t d_model, int64_t ldx,

@@ -90,7 +90,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else _vp(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _require(cond: bool, message: str):
@@ -135,8 +135,12 @@ def _row_stride(t) -> int:
     return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
 
 
-def _stream_handle(device) -> _vp:
-    return _vp(torch.cuda.current_stream(device).cuda_stream)
+# The current stream's handle by itself where torch has it: a Stream object around it takes 2 us, a sixth of a small call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_handle(device) -> int:
+    return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 class Camera:
@@ -385,10 +389,14 @@ class Camera:
         return out
 
     # ---- judging and repairing a pruned model ------------------------------
-    @staticmethod
-    def _check_logits(logits, per_row=()):
+    def _check_here(self, t, name: str):
+        if t.device != self.device:
+            _require(False, f"{name}: on {t.device}, the context is on {self.device}")
+
+    def _check_logits(self, logits, per_row=()):
         """Logits as a matrix, and float32 / int32 tensors with a value (or a fixed number of values) for every row of it."""
         _check_matrix(logits, "logits")
+        self._check_here(logits, "logits")
         for t, name, dtype, shape in per_row:
             if t is None:
                 continue
@@ -471,9 +479,9 @@ class Camera:
             (ACCUMULATE if accumulate else 0) | (DISTILL_TAIL if tail else 0), _ptr(dlogits), _row_stride(dlogits)))
         return dlogits
 
-    @staticmethod
-    def _check_gated(X, W_gate, W_up):
+    def _check_gated(self, X, W_gate, W_up):
         _check_matrix(X, "X")
+        self._check_here(X, "X")
         for t, name in ((W_gate, "W_gate"), (W_up, "W_up")):
             _check_matrix(t, name, like=X)
             _check_flat(t, name)
@@ -483,7 +491,8 @@ class Camera:
     def gated_ffn(self, X, W_gate, W_up, want_pre=False, H=None):
         """H [n, d_ff] = silu(X W_gate^T) * (X W_up^T) for the micro-experts of one expert: X [n, d_model], W_gate, W_up
         [d_ff, d_model].  want_pre: returns (H, pre), pre [n, 2, P] float32 the two projections that the backward call takes.
-        H allocated here has rows of a whole number of 16-byte vectors (a view of the first d_ff columns)."""
+        H allocated here has rows of a whole number of 16-byte vectors (a view of the first d_ff columns).  In a given H the columns
+        from d_ff to the next whole vector are set to zero."""
         self._check_gated(X, W_gate, W_up)
         n, d_ff = X.shape[0], W_gate.shape[0]
         v = 16 // X.element_size()

@@ -162,6 +162,24 @@ def test_gradient_against_differences(cam):
         assert float((got.double() - want).abs().max()) < 1e-8 + 400 * U
 
 
+def test_operands_beyond_32_bit_offsets(cam):
+    """The rows of [dG | dU], and those of their transpose, are more than 2 GiB; the last rows of every result against the definition."""
+    n, d, f = 30000, 8, 18000
+    X, Wg, Wu, _ = make(n, d, f, "bf16", 11)
+    dH = torch.randn((n, f), generator=torch.Generator(device="cuda").manual_seed(12), device="cuda", dtype=torch.bfloat16)
+    H, pre = cam.gated_ffn(X, Wg, Wu, want_pre=True)
+    dX, dWg, dWu = cam.gated_ffn_backward(X, Wg, Wu, dH, pre=pre)
+    torch.cuda.synchronize()
+    few = slice(n - 40, n)
+    w = reference(X[few], Wg, Wu, dH[few], "bf16")
+    close(H[few], *w["H"], "bf16", "H")
+    close(dX[few], *w["dX"], "bf16", "dX")
+    few = slice(f - 40, f)
+    w = reference(X, Wg[few], Wu[few], dH[:, few], "bf16")
+    close(dWg[few], *w["dW_gate"], "bf16", "dW_gate")
+    close(dWu[few], *w["dW_up"], "bf16", "dW_up")
+
+
 def test_packed_expert(cam):
     """The rows that a pruning leaves of one expert, where they lie in the packed matrices."""
     g = torch.Generator(device="cuda").manual_seed(3)
@@ -223,6 +241,6 @@ def test_binding_refuses_what_the_library_cannot_see(cam):
     X, Wg, Wu, dH = make(4, 64, 24, "bf16", 1)
     for call in (lambda: cam.gated_ffn(X, Wg.t(), Wu.t()), lambda: cam.gated_ffn(X, Wg, Wu[:20]), lambda: cam.gated_ffn(X, Wg.float(), Wu.float()),
                  lambda: cam.gated_ffn(X[:, ::2], Wg, Wu), lambda: cam.gated_ffn(X, Wg, Wu, H=torch.empty((4, 23), dtype=X.dtype, device="cuda")),
-                 lambda: cam.gated_ffn_backward(X, Wg, Wu, dH[:, :20]), lambda: cam.gated_ffn_backward(X, Wg, Wu, dH, pre=dH.float())):
+                 lambda: cam.gated_ffn(X.cpu(), Wg.cpu(), Wu.cpu()), lambda: cam.gated_ffn_backward(X, Wg, Wu, dH[:, :20]), lambda: cam.gated_ffn_backward(X, Wg, Wu, dH, pre=dH.float())):
         with pytest.raises(binding.CameraError):
             call()

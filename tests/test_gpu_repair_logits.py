@@ -506,7 +506,8 @@ def test_no_rows(cam):
 def test_binding_refuses_what_the_library_cannot_see(cam):
     z = make_logits(4, 100, "f32", 1)
     idx, val = make_teacher(4, 100, 3, 1.0, 2, True)
-    for call in (lambda: cam.token_logprobs(z.t()), lambda: cam.token_logprobs(z, torch.zeros(3, dtype=torch.int32, device="cuda")),
+    for call in (lambda: cam.token_logprobs(z.t()), lambda: cam.token_logprobs(z.cpu()), lambda: cam.distill_topk(z.cpu(), idx.cpu(), val.cpu()),
+                 lambda: cam.token_logprobs_backward(z, None, torch.zeros((4, 2), device="cuda"), torch.zeros(4), dlogits=z.cpu()), lambda: cam.token_logprobs(z, torch.zeros(3, dtype=torch.int32, device="cuda")),
                  lambda: cam.token_logprobs(z, torch.zeros(4, dtype=torch.int64, device="cuda")),
                  lambda: cam.distill_topk(z, idx[:, ::2], val[:, ::2]), lambda: cam.distill_topk(z, idx, val.double()),
                  lambda: cam.token_logprobs_backward(z, None, torch.zeros((4, 2), device="cuda"), None),
