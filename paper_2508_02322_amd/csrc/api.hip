@@ -1101,7 +1101,7 @@ int check_dlogits(camera_ctx* ctx, const void* logits, int dtype, int64_t n, int
   if (!aligned_to(dlogits, dtype == CAMERA_BF16 ? 2 : 4)) return fail(ctx, CAMERA_ESHAPE, "dlogits: not aligned to an element");
   if (dlogits == logits && (accumulate || ldd != ld))
     return fail(ctx, CAMERA_EINVAL, "dlogits: may be logits only with the same stride and without CAMERA_ACCUMULATE");
-  if (n * (int64_t)camera::logit_grad_parts(dtype, vocab) >= (int64_t(1) << 31))
+  if (n * (int64_t)camera::logit_grad_plan(dtype, vocab).parts >= (int64_t(1) << 31))
     return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
   return CAMERA_OK;
 }
@@ -1128,11 +1128,11 @@ int camera_token_logprobs(camera_ctx* ctx, void* stream_, const void* logits, in
   if (!aligned_to(targets, 4) || !aligned_to(logprob, 4) || !aligned_to(entropy, 4) || !aligned_to(stats, 4) ||
       !aligned_to(top_idx, 4) || !aligned_to(top_logprob, 4))
     return fail(ctx, CAMERA_ESHAPE, "targets / outputs: not aligned to an element");
-  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, false);
+  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, false, top_k);
   if (n * plan.parts >= (int64_t(1) << 31)) return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
   if (n == 0) return CAMERA_OK;
 
-  camera::LogprobArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, top_k, reciprocal(temperature), targets,
+  camera::LogprobArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, plan.threads, top_k, reciprocal(temperature), targets,
                         logprob, entropy, stats, top_idx, top_logprob, nullptr, nullptr};
   Carver cv;
   const size_t most = (size_t)std::max<int64_t>(plan.parts > 1 ? n * plan.parts : 0, camera::kLogitParts);
@@ -1163,7 +1163,8 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream_, const void* l
     return fail(ctx, CAMERA_ESHAPE, "targets / stats / entropy / gradients: not aligned to an element");
   if (n == 0) return CAMERA_OK;
 
-  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, camera::logit_grad_parts(dtype, vocab), flags & CAMERA_ACCUMULATE,
+  const camera::LogitPlan plan = camera::logit_grad_plan(dtype, vocab);
+  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, plan.parts, plan.threads, flags & CAMERA_ACCUMULATE,
                                 reciprocal(temperature), stats};
   DeviceGuard guard;
   CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
@@ -1184,11 +1185,11 @@ int camera_distill_topk(camera_ctx* ctx, void* stream_, const void* logits, int 
   if (n > 0 && (loss == nullptr || stats == nullptr)) return fail(ctx, CAMERA_EINVAL, "loss / stats: NULL");
   if (!aligned_to(loss, 4) || !aligned_to(stats, 4)) return fail(ctx, CAMERA_ESHAPE, "loss / stats: not aligned to an element");
   const int tail = flags & CAMERA_DISTILL_TAIL;
-  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, tail != 0);
+  const camera::LogitPlan plan = camera::logit_plan(dtype, n, vocab, tail != 0, 0);
   if (n * plan.parts >= (int64_t(1) << 31)) return fail(ctx, CAMERA_EUNSUPPORTED, "n * vocab: too large for one call");
   if (n == 0) return CAMERA_OK;
 
-  camera::DistillArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, tail, temperature, {teacher_idx, teacher_logprob, k}, loss, stats, nullptr};
+  camera::DistillArgs a{logits, ld, n, vocab, plan.part_len, plan.parts, plan.threads, tail, temperature, {teacher_idx, teacher_logprob, k}, loss, stats, nullptr};
   const size_t most = (size_t)std::max<int64_t>(plan.parts > 1 ? n * plan.parts : 0, camera::kLogitParts);
   DeviceGuard guard;
   CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");
@@ -1213,7 +1214,8 @@ int camera_distill_topk_backward(camera_ctx* ctx, void* stream_, const void* log
   if (!aligned_to(stats, 4) || !aligned_to(grad_loss, 4)) return fail(ctx, CAMERA_ESHAPE, "stats / grad_loss: not aligned to an element");
   if (n == 0) return CAMERA_OK;
 
-  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, camera::logit_grad_parts(dtype, vocab), flags & CAMERA_ACCUMULATE,
+  const camera::LogitPlan plan = camera::logit_grad_plan(dtype, vocab);
+  const camera::LogitGradArgs a{logits, ld, dlogits, ldd, n, vocab, plan.parts, plan.threads, flags & CAMERA_ACCUMULATE,
                                 reciprocal(temperature), stats};
   DeviceGuard guard;
   CAMERA_HIP(guard.enter(ctx->device), "hipSetDevice");

@@ -271,13 +271,14 @@ constexpr int kLogitParts = 1024;     // workgroups that a launch is cut into: a
 struct LogitPlan {
   int parts;
   int64_t part_len;
+  int threads;  // of a workgroup
 };
 // marks: a part's tokens have a bit each in LDS (distillation with the unlisted tokens as a class)
-LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks);
+LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks, int top_k);
 struct LogprobArgs {
   const void* logits;
   int64_t ld, n, vocab, part_len;
-  int parts, top_k;
+  int parts, threads, top_k;
   float inv_temperature;
   const int32_t* targets;
   float *logprob, *entropy, *stats;
@@ -292,12 +293,12 @@ struct LogitGradArgs {
   int64_t ld;
   void* dlogits;         // may be logits, with the same stride
   int64_t ldd, n, vocab;
-  int parts;             // logit_grad_parts
+  int parts, threads;    // logit_grad_plan
   int accumulate;
   float inv_temperature;
   const float* stats;
 };
-int logit_grad_parts(int dtype, int64_t vocab);
+LogitPlan logit_grad_plan(int dtype, int64_t vocab);
 hipError_t launch_token_logprobs_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const int32_t* targets,
                                       const float* entropy, const float* grad_logprob, const float* grad_entropy);
 struct DistillTeacher {
@@ -308,7 +309,7 @@ struct DistillTeacher {
 struct DistillArgs {
   const void* logits;
   int64_t ld, n, vocab, part_len;
-  int parts, tail;
+  int parts, threads, tail;
   float temperature;
   DistillTeacher teacher;
   float *loss, *stats;

@@ -18,12 +18,13 @@
 namespace camera {
 namespace {
 
-constexpr int kThreads = 512;  // >= CAMERA_MAX_ALTERNATIVES: the k-th largest of the threads' maxima exists
-constexpr int kWaves = kThreads / kWave;
+// Threads of a workgroup (TH below): kLong, or kShort where many short rows would leave most of the threads without a vector.
+constexpr int kLong = 512, kShort = 128;
+constexpr int kShortVocab = 16384, kShortTop = 64;  // longest row and most alternatives for the short workgroup
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kFloor = -1.0e4f;  // exponents are clamped here: exp2 of it is 0, and 0 times it is 0
-static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "one thread for every alternative");
+static_assert(kLong >= CAMERA_MAX_ALTERNATIVES && kShort >= kShortTop, "the k-th largest of the threads' maxima exists");
 
 // 16 bytes of a row.  Rows start where the caller's do, at any element: the loads and stores carry the element's alignment only.
 template <class T>
@@ -77,8 +78,8 @@ __device__ __forceinline__ X wave_all(X x, F f) {
   for (int d = 1; d < kWave; d <<= 1) x = f(x, __shfl_xor(x, d));
   return x;
 }
-// Every thread gets the result, taken in the same order; slots: kWaves values of LDS.  Barriers inside.
-template <class X, class F>
+// Every thread gets the result, taken in the same order; slots: a value of LDS per wave.  Barriers inside.
+template <int TH, class X, class F>
 __device__ __forceinline__ X block_all(X x, F f, X* slots) {
   x = wave_all(x, f);
   __syncthreads();  // the slots' earlier use is over
@@ -86,7 +87,7 @@ __device__ __forceinline__ X block_all(X x, F f, X* slots) {
   __syncthreads();
   X all = slots[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) all = f(all, slots[w]);
+  for (int w = 1; w < TH / kWave; ++w) all = f(all, slots[w]);
   return all;
 }
 struct Add {
@@ -129,12 +130,13 @@ __device__ __forceinline__ float add_values(Running& r, const float* z, float sc
   return largest;
 }
 struct Slots {
-  float f[2][kWaves];
+  float f[2][kLong / kWave];
 };
+template <int TH>
 __device__ __forceinline__ Running block_running(Running r, float scale, Slots& slots) {
-  rescale(r, block_all(r.m, Max{}, slots.f[0]), scale);
-  r.s = block_all(r.s, Add{}, slots.f[1]);
-  r.t = block_all(r.t, Add{}, slots.f[0]);
+  rescale(r, block_all<TH>(r.m, Max{}, slots.f[0]), scale);
+  r.s = block_all<TH>(r.s, Add{}, slots.f[1]);
+  r.t = block_all<TH>(r.t, Add{}, slots.f[0]);
   return r;
 }
 
@@ -153,11 +155,11 @@ __device__ __forceinline__ uint64_t make_key(uint32_t bits, int index) { return 
 __device__ __forceinline__ int key_index(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
 
 // ---- one part of a row ---------------------------------------------------------------------------------------------
-// Thread j's stripe is the vectors j, j + kThreads, ... of the part, and element j of what is left behind the whole vectors.  A
+// Thread j's stripe is the vectors j, j + TH, ... of the part, and element j of what is left behind the whole vectors.  A
 // stripe is cut into cells of per_cell groups of kUnroll vectors (what is left belongs to the last one).
 constexpr int kUnroll = 4;  // vectors in flight per thread
 constexpr int kCells = 16;
-template <class T>
+template <class T, int TH>
 struct RowPart {
   static constexpr int N = Pack<T>::N;
   using Raw = typename Pack<T>::Raw;
@@ -166,7 +168,7 @@ struct RowPart {
   int vecs, rest;
   int per_cell, cells;
   __device__ RowPart(const T* row, int64_t first_, int len) : z(row + first_), first((int)first_), vecs(len / N), rest(len % N) {
-    const int groups = (vecs + kUnroll * kThreads - 1) / (kUnroll * kThreads);
+    const int groups = (vecs + kUnroll * TH - 1) / (kUnroll * TH);
     per_cell = groups / kCells + 1;
     cells = groups / per_cell + 1;  // <= kCells
   }
@@ -174,13 +176,13 @@ struct RowPart {
   __device__ __forceinline__ float left(int i) const { return Pack<T>::one(z[(int64_t)vecs * N + i]); }
 };
 
-// Marks of a part's listed elements, a bit each.
-constexpr int kMaxListed = 1 << 18;  // elements of a part with marks: 32 KiB of LDS, four workgroups a compute unit
+// Marks of a part's listed elements, a bit each: 32 KiB of LDS for the long workgroup, four of them a compute unit.
+constexpr int kMaxListed = 1 << 18;
 
 // The thread's sums over its stripe.  cell_max (CELLS): upper half of the order bits of every cell's largest value, [cell][thread].
 // meanwhile(): done once the first loads are under way.
-template <class T, bool ENTROPY, bool LISTED, bool CELLS, class F>
-__device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale, const unsigned char* marks, uint16_t* cell_max, F&& meanwhile) {
+template <bool ENTROPY, bool LISTED, bool CELLS, class T, int TH, class F>
+__device__ __forceinline__ Running stream_part(const RowPart<T, TH>& p, float scale, const unsigned char* marks, uint16_t* cell_max, F&& meanwhile) {
   constexpr int N = Pack<T>::N, U = kUnroll;
   const int tid = threadIdx.x;
   Running r;
@@ -201,18 +203,18 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
   auto fetch = [&] {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (v + u * kThreads < p.vecs) raw[u] = p.load(v + u * kThreads);
+      if (v + u * TH < p.vecs) raw[u] = p.load(v + u * TH);
   };
   fetch();
   meanwhile();
-  for (; v + (U - 1) * kThreads < p.vecs; v += U * kThreads, fetch()) {
+  for (; v + (U - 1) * TH < p.vecs; v += U * TH, fetch()) {
     float z[U * N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) one(raw[u], v + u * kThreads, z + u * N);
+    for (int u = 0; u < U; ++u) one(raw[u], v + u * TH, z + u * N);
     largest = fmaxf(largest, add_values<ENTROPY, U * N>(r, z, scale));
     if constexpr (CELLS) {
       if (++groups == p.per_cell) {
-        cell_max[cell++ * kThreads + tid] = (uint16_t)(order_bits(largest) >> 16);
+        cell_max[cell++ * TH + tid] = (uint16_t)(order_bits(largest) >> 16);
         largest = -INFINITY;
         groups = 0;
       }
@@ -220,15 +222,15 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
   }
 #pragma unroll
   for (int u = 0; u < U - 1; ++u)  // up to three vectors are left
-    if (v + u * kThreads < p.vecs) {
+    if (v + u * TH < p.vecs) {
       float z[N];
-      one(raw[u], v + u * kThreads, z);
+      one(raw[u], v + u * TH, z);
       largest = fmaxf(largest, add_values<ENTROPY, N>(r, z, scale));
     }
   if constexpr (CELLS) {
     for (; cell < p.cells; ++cell) {
       if (cell == p.cells - 1 && tid < p.rest) largest = fmaxf(largest, p.left(tid));
-      cell_max[cell * kThreads + tid] = (uint16_t)(order_bits(largest) >> 16);
+      cell_max[cell * TH + tid] = (uint16_t)(order_bits(largest) >> 16);
       largest = -INFINITY;
     }
   }
@@ -244,14 +246,15 @@ __device__ __forceinline__ Running stream_part(const RowPart<T>& p, float scale,
 }
 
 // ---- the largest k -------------------------------------------------------------------------------------------------
-constexpr int kCandidates = 2048;  // >= the elements of a part that has fewer stripes than alternatives are wanted
-constexpr int kChosen = 1024;
 // Up to this many candidates are placed by counting the larger ones (their square, over the workgroup's lanes), more by sorting.
 constexpr int kCounted = 128;
+template <int TH>
 struct SelectSmem {
-  uint32_t largest[kThreads];
-  uint16_t cell_max[kCells * kThreads];  // of the rows' cells
-  int32_t chosen[kChosen];               // cells that may hold candidates: cell * kThreads + stripe
+  // as many candidates as a part has elements that has fewer stripes than alternatives are wanted
+  static constexpr int kCandidates = 8 * (TH == kLong ? CAMERA_MAX_ALTERNATIVES : kShortTop), kChosen = 2 * TH;
+  uint32_t largest[TH];
+  uint16_t cell_max[kCells * TH];  // of the rows' cells
+  int32_t chosen[kChosen];         // cells that may hold candidates: cell * TH + stripe
   uint64_t keys[kCandidates];
   int32_t hist[256];
   uint32_t bound;
@@ -261,9 +264,9 @@ struct SelectSmem {
 };
 
 // Where keys come from: every stripe has cells() cells of positions() places of up to N keys.
-template <class T>
+template <class T, int TH>
 struct LogitKeys {
-  const RowPart<T>& p;
+  const RowPart<T, TH>& p;
   __device__ __forceinline__ int cells() const { return p.cells; }
   __device__ __forceinline__ int positions() const { return p.per_cell * kUnroll + (p.rest != 0 ? 1 : 0); }
   template <class F>
@@ -271,7 +274,7 @@ struct LogitKeys {
     constexpr int N = Pack<T>::N;
     const int whole = p.per_cell * kUnroll;
     if (pos < whole) {
-      const int v = (cell * whole + pos) * kThreads + stripe;
+      const int v = (cell * whole + pos) * TH + stripe;
       if (v < p.vecs) {
         float z[N];
         Pack<T>::get(p.load(v), z);
@@ -283,14 +286,15 @@ struct LogitKeys {
     }
   }
 };
+template <int TH>
 struct ListKeys {
   const uint64_t* keys;
   int n;
   __device__ __forceinline__ int cells() const { return 1; }
-  __device__ __forceinline__ int positions() const { return (n + kThreads - 1) / kThreads; }
+  __device__ __forceinline__ int positions() const { return (n + TH - 1) / TH; }
   template <class F>
   __device__ __forceinline__ void at(int stripe, int, int pos, F&& f) const {
-    const int i = pos * kThreads + stripe;
+    const int i = pos * TH + stripe;
     if (i < n) {
       const uint64_t key = keys[i];
       f((uint32_t)(key >> 32), key_index(key));
@@ -306,8 +310,10 @@ struct ListKeys {
 // keys are all different, so the order in which candidates are found does not show.  Where more values
 // reach the bound than there is room for (ties: a constant row, a mask by the type's lowest value), the k-th largest key is
 // found by its digits, eight passes over the source.
-template <class SOURCE, class OUT>
-__device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem& sm, OUT&& out) {
+template <int TH, class SOURCE, class OUT>
+__device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem<TH>& sm, OUT&& out) {
+  constexpr int kWaves = TH / kWave, kCandidates = SelectSmem<TH>::kCandidates, kChosen = SelectSmem<TH>::kChosen;
+  static_assert(TH >= kCounted, "a thread for every counted candidate");
   const int tid = threadIdx.x, cells = src.cells(), positions = src.positions();
   sm.largest[tid] = largest;
   if (tid == 0) {
@@ -332,10 +338,10 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
   __syncthreads();
   const uint32_t bound = sm.bound;
   for (int c = 0; c < cells; ++c) {
-    const uint32_t m = sm.cell_max[c * kThreads + tid];
+    const uint32_t m = sm.cell_max[c * TH + tid];
     if (m >= bound >> 16 && m != 0) {
       const int at = atomicAdd(&sm.n_chosen, 1);
-      if (at < kChosen) sm.chosen[at] = c * kThreads + tid;
+      if (at < kChosen) sm.chosen[at] = c * TH + tid;
     }
   }
   __syncthreads();
@@ -345,9 +351,9 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
     if (at < kCandidates) sm.keys[at] = key;
   };
   if (n_chosen <= kChosen) {
-    for (int w = tid; w < n_chosen * positions; w += kThreads) {
+    for (int w = tid; w < n_chosen * positions; w += TH) {
       const int c = sm.chosen[w % n_chosen];
-      src.at(c % kThreads, c / kThreads, w / n_chosen, [&](uint32_t bits, int index) {
+      src.at(c % TH, c / TH, w / n_chosen, [&](uint32_t bits, int index) {
         if (bits >= bound && bits != 0) add_key(make_key(bits, index));
       });
     }
@@ -366,7 +372,7 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
     int want = k;
     for (int shift = 56; shift >= 0; shift -= 8) {
       __syncthreads();
-      if (tid < 256) sm.hist[tid] = 0;
+      for (int i = tid; i < 256; i += TH) sm.hist[i] = 0;
       __syncthreads();
       every([&](uint64_t key) {
         if (shift < 56 && (key ^ prefix) >> (shift + 8) != 0) return;
@@ -406,20 +412,20 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
   } else {
     int size = 2 * kCounted;
     while (size < n_keys) size *= 2;
-    for (int i = n_keys + tid; i < size; i += kThreads) sm.keys[i] = 0;
+    for (int i = n_keys + tid; i < size; i += TH) sm.keys[i] = 0;
     __syncthreads();
     for (int run = 2; run <= size; run *= 2)
       for (int apart = run / 2; apart > 0; apart /= 2) {
-        for (int c = tid; c < size / 2; c += kThreads) {
+        for (int c = tid; c < size / 2; c += TH) {
           const int i = 2 * c - (c & (apart - 1)), j = i + apart;  // the pairs `apart` from each other
           const uint64_t x = sm.keys[i], y = sm.keys[j];
           if ((x < y) == ((i & run) == 0)) sm.keys[i] = y, sm.keys[j] = x;
         }
         __syncthreads();
       }
-    for (int r = tid; r < min(k, n_keys); r += kThreads) out(r, sm.keys[r]);
+    for (int r = tid; r < min(k, n_keys); r += TH) out(r, sm.keys[r]);
   }
-  for (int r = n_keys + tid; r < k; r += kThreads) out(r, (uint64_t)0);
+  for (int r = n_keys + tid; r < k; r += TH) out(r, (uint64_t)0);
 }
 
 // ---- log probabilities, entropy, alternatives ----------------------------------------------------------------------
@@ -452,28 +458,28 @@ __device__ __forceinline__ void write_alternative(const LogprobArgs& a, const Ru
 }
 
 // A workgroup has a part of a row; with one part a row it ends it, else it leaves its sums and its alternatives' keys.
-template <class T, bool TOP>
-__global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(LogprobArgs a) {
+template <class T, int TH, bool TOP>
+__global__ __launch_bounds__(TH, 4) void logprobs_kernel(LogprobArgs a) {
   __shared__ Slots slots;
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
   const int part = (int)(block - row * a.parts);
   const int64_t first = part * a.part_len;
-  const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, (int)min(a.part_len, a.vocab - first));
+  const RowPart<T, TH> p(static_cast<const T*>(a.logits) + row * a.ld, first, (int)min(a.part_len, a.vocab - first));
   const float scale = a.inv_temperature * kLog2e;
-  SelectSmem* select = nullptr;
+  SelectSmem<TH>* select = nullptr;
   if constexpr (TOP) {
-    __shared__ SelectSmem sm;
+    __shared__ SelectSmem<TH> sm;
     select = &sm;
   }
-  const Running mine = stream_part<T, true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr, [] {});
-  const Running r = block_running(mine, scale, slots);
+  const Running mine = stream_part<true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr, [] {});
+  const Running r = block_running<TH>(mine, scale, slots);
   if (a.parts == 1) finish_logprobs<T>(r, a, row);
   else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
   if constexpr (TOP) {
     const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
-    select_top(LogitKeys<T>{p}, order_bits(mine.m), a.top_k, *select, [&](int place, uint64_t key) {
+    select_top<TH>(LogitKeys<T, TH>{p}, order_bits(mine.m), a.top_k, *select, [&](int place, uint64_t key) {
       if (a.parts == 1) write_alternative(a, r, log_sum, row, place, key);
       else a.part_keys[block * a.top_k + place] = key;
     });
@@ -481,9 +487,10 @@ __global__ __launch_bounds__(kThreads, 4) void logprobs_kernel(LogprobArgs a) {
 }
 
 // A row's parts put together, in their order.
+template <int TH>
 __device__ __forceinline__ Running join_parts(const float4* part_stats, int parts, float scale, Slots& slots) {
   Running mine;
-  for (int i = threadIdx.x; i < parts; i += kThreads) {
+  for (int i = threadIdx.x; i < parts; i += TH) {
     const float4 s = part_stats[i];
     Running other;
     other.m = s.x;
@@ -495,33 +502,34 @@ __device__ __forceinline__ Running join_parts(const float4* part_stats, int part
     mine.s += other.s;
     mine.t += other.t;
   }
-  return block_running(mine, scale, slots);
+  return block_running<TH>(mine, scale, slots);
 }
 template <class T, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprobs_join_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(kLong) void logprobs_join_kernel(LogprobArgs a) {
+  constexpr int TH = kLong;
   __shared__ Slots slots;
   const int64_t row = linear_block();
   if (row >= a.n) return;
   const float scale = a.inv_temperature * kLog2e;
-  const Running r = join_parts(a.part_stats + row * a.parts, a.parts, scale, slots);
+  const Running r = join_parts<TH>(a.part_stats + row * a.parts, a.parts, scale, slots);
   finish_logprobs<T>(r, a, row);
   if constexpr (TOP) {
-    __shared__ SelectSmem sm;
+    __shared__ SelectSmem<TH> sm;
     const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
-    const ListKeys keys{a.part_keys + row * a.parts * a.top_k, a.parts * a.top_k};
+    const ListKeys<TH> keys{a.part_keys + row * a.parts * a.top_k, a.parts * a.top_k};
     uint32_t largest = 0;
     for (int pos = 0; pos < keys.positions(); ++pos) keys.at(threadIdx.x, 0, pos, [&](uint32_t bits, int) { largest = max(largest, bits); });
     sm.cell_max[threadIdx.x] = (uint16_t)(largest >> 16);
-    select_top(keys, largest, a.top_k, sm, [&](int place, uint64_t key) { write_alternative(a, r, log_sum, row, place, key); });
+    select_top<TH>(keys, largest, a.top_k, sm, [&](int place, uint64_t key) { write_alternative(a, r, log_sum, row, place, key); });
   }
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------------------
 // A workgroup has kGradVecs vectors of a row; every thread has its vectors' loads in flight together.
 constexpr int kGradUnroll = 4;
-template <class T>
+template <class T, int TH>
 struct GradPart {
-  static constexpr int N = Pack<T>::N, kLen = kThreads * kGradUnroll * N;
+  static constexpr int N = Pack<T>::N, kLen = TH * kGradUnroll * N;
   using Raw = typename Pack<T>::Raw;
   const T* z;
   T* out;
@@ -535,7 +543,7 @@ struct GradPart {
     const int vecs = len / N, tid = threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
-      const int v = tid + u * kThreads;
+      const int v = tid + u * TH;
       if (v < vecs) {
         raw[u] = *reinterpret_cast<const Raw*>(z + v * N);
         if (accumulate) old[u] = *reinterpret_cast<const Raw*>(out + v * N);
@@ -548,7 +556,7 @@ struct GradPart {
     const int vecs = len / N, rest = len - vecs * N, tid = threadIdx.x;
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
-      const int v = tid + u * kThreads;
+      const int v = tid + u * TH;
       if (v < vecs) {
         float x[N];
         Pack<T>::get(raw[u], x);
@@ -572,15 +580,15 @@ struct GradPart {
   }
   __device__ __forceinline__ void zero() const {
     const int vecs = len / N, rest = len - vecs * N;
-    for (int v = threadIdx.x; v < vecs; v += kThreads) *reinterpret_cast<Raw*>(out + v * N) = Raw{0, 0, 0, 0};
+    for (int v = threadIdx.x; v < vecs; v += TH) *reinterpret_cast<Raw*>(out + v * N) = Raw{0, 0, 0, 0};
     if ((int)threadIdx.x < rest) out[vecs * N + threadIdx.x] = Pack<T>::round(0.0f);
   }
 };
-template <class T>
-__device__ __forceinline__ GradPart<T> grad_part(const LogitGradArgs& a, int64_t row, int part) {
-  GradPart<T> p;
-  p.first = (int64_t)part * GradPart<T>::kLen;
-  p.len = (int)min((int64_t)GradPart<T>::kLen, a.vocab - p.first);
+template <class T, int TH>
+__device__ __forceinline__ GradPart<T, TH> grad_part(const LogitGradArgs& a, int64_t row, int part) {
+  GradPart<T, TH> p;
+  p.first = (int64_t)part * p.kLen;
+  p.len = (int)min((int64_t)p.kLen, a.vocab - p.first);
   p.z = static_cast<const T*>(a.logits) + row * a.ld + p.first;
   p.out = static_cast<T*>(a.dlogits) + row * a.ldd + p.first;
   p.accumulate = a.accumulate != 0;
@@ -588,15 +596,15 @@ __device__ __forceinline__ GradPart<T> grad_part(const LogitGradArgs& a, int64_t
 }
 
 // d logprob[t] / dz_v = (1[v = t] - p_v) / T,  d H / dz_v = -p_v (log p_v + H) / T
-template <class T>
-__global__ __launch_bounds__(kThreads) void logprobs_grad_kernel(LogitGradArgs a, const int32_t* __restrict__ targets,
+template <class T, int TH>
+__global__ __launch_bounds__(TH) void logprobs_grad_kernel(LogitGradArgs a, const int32_t* __restrict__ targets,
                                                                  const float* __restrict__ entropy,
                                                                  const float* __restrict__ grad_logprob,
                                                                  const float* __restrict__ grad_entropy) {
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
-  GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  GradPart<T, TH> p = grad_part<T, TH>(a, row, (int)(block - row * a.parts));
   const int64_t target = targets ? (int64_t)targets[row] : -1;
   const float m = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
   const float one = grad_logprob && target >= 0 && target < a.vocab ? grad_logprob[row] * a.inv_temperature : 0.0f;
@@ -636,30 +644,45 @@ struct TeacherSmem {
   __align__(16) int32_t id[CAMERA_MAX_ALTERNATIVES];
   float value[CAMERA_MAX_ALTERNATIVES];
 };
+template <int TH>
 __device__ __forceinline__ void load_teacher(const DistillTeacher& t, int64_t row, int64_t vocab, TeacherSmem& sm) {
-  static_assert(kThreads >= CAMERA_MAX_ALTERNATIVES, "a thread for every entry");
-  const int j = threadIdx.x, padded = (t.k + 3) & ~3;
-  int32_t id = -1;
-  if (j < padded) {
-    float value = -INFINITY;
-    if (j < t.k) {
-      id = t.idx[row * t.k + j];
-      value = t.logprob[row * t.k + j];
-    }
-    sm.id[j] = id;
-    sm.value[j] = value;
-    if (id < 0 || id >= vocab || !(value > -INFINITY)) id = -1;
-  }
-  __syncthreads();
-  bool repeats = false;
-  if (j < padded) {
-    for (int i = 0; i < padded; i += 4) {  // whole vectors, no early end: the reads follow each other without waiting
-      const int4 other = *reinterpret_cast<const int4*>(&sm.id[i]);
-      repeats = repeats || (other.x == id && i < j) || (other.y == id && i + 1 < j) || (other.z == id && i + 2 < j) || (other.w == id && i + 3 < j);
+  constexpr int kEach = (CAMERA_MAX_ALTERNATIVES + TH - 1) / TH;  // entries of a thread
+  const int padded = (t.k + 3) & ~3;
+  int32_t id[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = threadIdx.x + e * TH;
+    id[e] = -1;
+    if (j < padded) {
+      float value = -INFINITY;
+      if (j < t.k) {
+        id[e] = t.idx[row * t.k + j];
+        value = t.logprob[row * t.k + j];
+      }
+      sm.id[j] = id[e];
+      sm.value[j] = value;
+      if (id[e] < 0 || id[e] >= vocab || !(value > -INFINITY)) id[e] = -1;
     }
   }
   __syncthreads();
-  if (j < padded && (repeats || id < 0)) sm.id[j] = -1;
+  bool repeats[kEach] = {};
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = threadIdx.x + e * TH;
+    if (j < padded) {
+      for (int i = 0; i < padded; i += 4) {  // whole vectors, no early end: the reads follow each other without waiting
+        const int4 other = *reinterpret_cast<const int4*>(&sm.id[i]);
+        repeats[e] = repeats[e] || (other.x == id[e] && i < j) || (other.y == id[e] && i + 1 < j) || (other.z == id[e] && i + 2 < j) ||
+                     (other.w == id[e] && i + 3 < j);
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = threadIdx.x + e * TH;
+    if (j < padded && (repeats[e] || id[e] < 0)) sm.id[j] = -1;
+  }
   __syncthreads();
 }
 
@@ -737,8 +760,8 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
   }
 }
 
-template <class T, bool TAIL>
-__global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
+template <class T, int TH, bool TAIL>
+__global__ __launch_bounds__(TH, 4) void distill_kernel(DistillArgs a) {
   __shared__ Slots slots;
   __shared__ TeacherSmem teacher;
   const int64_t block = linear_block();
@@ -747,52 +770,53 @@ __global__ __launch_bounds__(kThreads, 4) void distill_kernel(DistillArgs a) {
   const int part = (int)(block - row * a.parts);
   const int64_t first = part * a.part_len;
   const int len = (int)min(a.part_len, a.vocab - first);
-  const RowPart<T> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
+  const RowPart<T, TH> p(static_cast<const T*>(a.logits) + row * a.ld, first, len);
   const float scale = kLog2e / a.temperature;
   Running mine;
   if constexpr (TAIL) {
-    __shared__ __align__(16) uint32_t marks[kMaxListed / 32];
-    mine = stream_part<T, false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr, [&] {
-      for (int i = threadIdx.x; i < (len + 31) / 32; i += kThreads) marks[i] = 0;
-      load_teacher(a.teacher, row, a.vocab, teacher);
-      for (int j = threadIdx.x; j < a.teacher.k; j += kThreads) {
+    __shared__ __align__(16) uint32_t marks[(TH == kLong ? kMaxListed : kShortVocab) / 32];
+    mine = stream_part<false, true, false>(p, scale, reinterpret_cast<const unsigned char*>(marks), nullptr, [&] {
+      for (int i = threadIdx.x; i < (len + 31) / 32; i += TH) marks[i] = 0;
+      load_teacher<TH>(a.teacher, row, a.vocab, teacher);
+      for (int j = threadIdx.x; j < a.teacher.k; j += TH) {
         const int64_t at = teacher.id[j] < 0 ? -1 : teacher.id[j] - first;
         if (at >= 0 && at < len) atomicOr(&marks[at >> 5], 1u << (at & 31));
       }
       __syncthreads();
     });
   } else {
-    mine = stream_part<T, false, false, false>(p, scale, nullptr, nullptr, [&] {
-      if (a.parts == 1) load_teacher(a.teacher, row, a.vocab, teacher);
+    mine = stream_part<false, false, false>(p, scale, nullptr, nullptr, [&] {
+      if (a.parts == 1) load_teacher<TH>(a.teacher, row, a.vocab, teacher);
     });
   }
-  const Running r = block_running(mine, scale, slots);
+  const Running r = block_running<TH>(mine, scale, slots);
   if (a.parts == 1) {
     if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
   } else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, 0.0f, 0.0f);
 }
 template <class T>
-__global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
+__global__ __launch_bounds__(kLong) void distill_join_kernel(DistillArgs a) {
+  constexpr int TH = kLong;
   __shared__ Slots slots;
   __shared__ TeacherSmem teacher;
   const int64_t row = linear_block();
   if (row >= a.n) return;
-  load_teacher(a.teacher, row, a.vocab, teacher);
-  const Running r = join_parts(a.part_stats + row * a.parts, a.parts, kLog2e / a.temperature, slots);
+  load_teacher<TH>(a.teacher, row, a.vocab, teacher);
+  const Running r = join_parts<TH>(a.part_stats + row * a.parts, a.parts, kLog2e / a.temperature, slots);
   if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
 }
 
 // d loss / dz_v = (mass p_v - q_v) / T for a listed v, p_v (mass - q_r / p_r) / T for an unlisted one (mass alone without tail):
 // the second for every token of the part, then the first over the listed ones.  A listed token's logit and old gradient
 // are read before anything is written (dlogits may be logits), and its value is written after the workgroup's stores are done.
-template <class T>
-__global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a, DistillTeacher teacher, int tail,
+template <class T, int TH>
+__global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, DistillTeacher teacher, int tail,
                                                                 const float* __restrict__ grad_loss) {
   __shared__ TeacherSmem list;
   const int64_t block = linear_block();
   const int64_t row = block / a.parts;
   if (row >= a.n) return;
-  GradPart<T> p = grad_part<T>(a, row, (int)(block - row * a.parts));
+  GradPart<T, TH> p = grad_part<T, TH>(a, row, (int)(block - row * a.parts));
   const float* st = a.stats + row * CAMERA_DISTILL_STATS;
   const float m = st[0], log_sum = st[1], norm = st[2], mass = st[3], log_ratio = st[4];
   const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
@@ -801,17 +825,23 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a,
     return;
   }
   p.fetch();  // in flight while the list is looked through
-  load_teacher(teacher, row, a.vocab, list);
-  const int j = threadIdx.x;
-  const int64_t at = j < teacher.k && list.id[j] >= 0 ? list.id[j] - p.first : -1;
-  const bool here = at >= 0 && at < p.len;
-  float listed = 0.0f;
-  if (here) {
-    const float value = list.value[j];
-    const float lp = fmaxf((Pack<T>::one(p.z[at]) - m) * inv_t - log_sum, kFloor);
-    const float lq = tail ? value : value * inv_t - norm;
-    listed = g * (mass * expf(lp) - expf(lq));
-    if (p.accumulate) listed += Pack<T>::one(p.out[at]);
+  load_teacher<TH>(teacher, row, a.vocab, list);
+  constexpr int kEach = (CAMERA_MAX_ALTERNATIVES + TH - 1) / TH;  // entries of a thread
+  int64_t at[kEach];
+  float listed[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int j = threadIdx.x + e * TH;
+    at[e] = j < teacher.k && list.id[j] >= 0 ? list.id[j] - p.first : -1;
+    if (at[e] >= p.len) at[e] = -1;
+    listed[e] = 0.0f;
+    if (at[e] >= 0) {
+      const float value = list.value[j];
+      const float lp = fmaxf((Pack<T>::one(p.z[at[e]]) - m) * inv_t - log_sum, kFloor);
+      const float lq = tail ? value : value * inv_t - norm;
+      listed[e] = g * (mass * expf(lp) - expf(lq));
+      if (p.accumulate) listed[e] += Pack<T>::one(p.out[at[e]]);
+    }
   }
   __syncthreads();  // the reads above are done before the part is written
   // p_v (mass - q_r / p_r) as one exponential: the ratio may be as large as p_r is small, and mass is then nothing beside it
@@ -823,75 +853,91 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(LogitGradArgs a,
     for (int i = 0; i < N; ++i) x[i] = c * __builtin_amdgcn_exp2f(fmaf(x[i] - m, scale2, log2_factor));
   });
   __syncthreads();  // and written before the listed tokens are
-  if (here) p.out[at] = Pack<T>::round(listed);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e)
+    if (at[e] >= 0) p.out[at[e]] = Pack<T>::round(listed[e]);
 }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 }  // namespace
 
-// Parts of a row: as many as give the chip kLogitParts workgroups, each with at least a vector for every thread.
-LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks) {
-  const int64_t vec = dtype == CAMERA_BF16 ? 8 : 4, least = kThreads * vec;
+// Parts of a row: as many as give the chip kLogitParts workgroups, each with at least a vector for every thread.  Many short rows
+// are left whole, in short workgroups.
+LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks, int top_k) {
+  const int64_t vec = dtype == CAMERA_BF16 ? 8 : 4, least = kLong * vec;
+  LogitPlan plan{1, vocab, kShort};
+  if (n >= kLogitParts && vocab <= kShortVocab && top_k <= kShortTop) return plan;
+  plan.threads = kLong;
   int64_t parts = std::max<int64_t>(1, kLogitParts / std::max<int64_t>(1, n));
   parts = std::min(parts, std::max<int64_t>(1, vocab / least));
   if (marks) parts = std::max(parts, (vocab + kMaxListed - 1) / kMaxListed);
   parts = std::max(parts, (vocab + (int64_t(1) << 30) - 1) >> 30);  // a part's elements are counted in 31 bits
-  LogitPlan plan;
   plan.part_len = round_up((vocab + parts - 1) / parts, least / 8);
   plan.parts = (int)((vocab + plan.part_len - 1) / plan.part_len);
   return plan;
 }
 
-#define CAMERA_BY_TYPE(dtype, CALL)    \
-  do {                                 \
-    if ((dtype) == CAMERA_BF16) {      \
-      using T = __bf16;                \
-      CALL;                            \
-    } else {                           \
-      using T = float;                 \
-      CALL;                            \
-    }                                  \
+// CALL with T and TH
+#define CAMERA_BY_TYPE(dtype, threads, CALL) \
+  do {                                       \
+    auto call = [&](auto type, auto th) {    \
+      using T = decltype(type);              \
+      constexpr int TH = decltype(th)::value; \
+      CALL;                                  \
+    };                                       \
+    using Short = std::integral_constant<int, kShort>; \
+    using Long = std::integral_constant<int, kLong>;   \
+    if ((dtype) == CAMERA_BF16) {            \
+      if ((threads) == kShort) call(__bf16{}, Short{}); \
+      else call(__bf16{}, Long{});           \
+    } else {                                 \
+      if ((threads) == kShort) call(float{}, Short{});  \
+      else call(float{}, Long{});            \
+    }                                        \
   } while (0)
 
 hipError_t launch_token_logprobs(hipStream_t stream, int dtype, const LogprobArgs& a) {
   const int64_t blocks = a.n * a.parts;
   if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  const dim3 block(kThreads);
-  CAMERA_BY_TYPE(dtype, {
-    if (a.top_k > 0) hipLaunchKernelGGL((logprobs_kernel<T, true>), launch_grid(blocks), block, 0, stream, a);
-    else hipLaunchKernelGGL((logprobs_kernel<T, false>), launch_grid(blocks), block, 0, stream, a);
+  if (a.threads == kShort ? a.parts != 1 || a.top_k > kShortTop : a.threads != kLong) return hipErrorInvalidValue;
+  CAMERA_BY_TYPE(dtype, a.threads, {
+    if (a.top_k > 0) hipLaunchKernelGGL((logprobs_kernel<T, TH, true>), launch_grid(blocks), dim3(TH), 0, stream, a);
+    else hipLaunchKernelGGL((logprobs_kernel<T, TH, false>), launch_grid(blocks), dim3(TH), 0, stream, a);
     if (a.parts > 1) {
-      if (a.top_k > 0) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), launch_grid(a.n), block, 0, stream, a);
-      else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), launch_grid(a.n), block, 0, stream, a);
+      if (a.top_k > 0) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), launch_grid(a.n), dim3(kLong), 0, stream, a);
+      else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), launch_grid(a.n), dim3(kLong), 0, stream, a);
     }
   });
   return hipGetLastError();
 }
 
-int logit_grad_parts(int dtype, int64_t vocab) {
-  const int64_t len = dtype == CAMERA_BF16 ? GradPart<__bf16>::kLen : GradPart<float>::kLen;
-  return (int)((vocab + len - 1) / len);
+LogitPlan logit_grad_plan(int dtype, int64_t vocab) {
+  const int64_t vec = dtype == CAMERA_BF16 ? 8 : 4;
+  LogitPlan plan{1, kShort * kGradUnroll * vec, kShort};
+  if (vocab > plan.part_len) plan = {1, kLong * kGradUnroll * vec, kLong};
+  plan.parts = (int)((vocab + plan.part_len - 1) / plan.part_len);
+  return plan;
 }
 
 hipError_t launch_token_logprobs_grad(hipStream_t stream, int dtype, const LogitGradArgs& a, const int32_t* targets,
                                       const float* entropy, const float* grad_logprob, const float* grad_entropy) {
   const int64_t blocks = a.n * a.parts;
   if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  CAMERA_BY_TYPE(dtype, hipLaunchKernelGGL((logprobs_grad_kernel<T>), launch_grid(blocks), dim3(kThreads), 0, stream, a, targets,
-                                           entropy, grad_logprob, grad_entropy));
+  CAMERA_BY_TYPE(dtype, a.threads, hipLaunchKernelGGL((logprobs_grad_kernel<T, TH>), launch_grid(blocks), dim3(TH), 0, stream, a, targets,
+                                                      entropy, grad_logprob, grad_entropy));
   return hipGetLastError();
 }
 
 hipError_t launch_distill(hipStream_t stream, int dtype, const DistillArgs& a) {
   const int64_t blocks = a.n * a.parts;
   if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
+  if (a.threads == kShort ? a.parts != 1 || a.vocab > kShortVocab : a.threads != kLong) return hipErrorInvalidValue;
   if (a.tail && a.part_len > kMaxListed) return hipErrorInvalidValue;
-  const dim3 block(kThreads);
-  CAMERA_BY_TYPE(dtype, {
-    if (a.tail) hipLaunchKernelGGL((distill_kernel<T, true>), launch_grid(blocks), block, 0, stream, a);
-    else hipLaunchKernelGGL((distill_kernel<T, false>), launch_grid(blocks), block, 0, stream, a);
-    if (a.parts > 1) hipLaunchKernelGGL((distill_join_kernel<T>), launch_grid(a.n), block, 0, stream, a);
+  CAMERA_BY_TYPE(dtype, a.threads, {
+    if (a.tail) hipLaunchKernelGGL((distill_kernel<T, TH, true>), launch_grid(blocks), dim3(TH), 0, stream, a);
+    else hipLaunchKernelGGL((distill_kernel<T, TH, false>), launch_grid(blocks), dim3(TH), 0, stream, a);
+    if (a.parts > 1) hipLaunchKernelGGL((distill_join_kernel<T>), launch_grid(a.n), dim3(kLong), 0, stream, a);
   });
   return hipGetLastError();
 }
@@ -900,8 +946,8 @@ hipError_t launch_distill_grad(hipStream_t stream, int dtype, const LogitGradArg
                                const float* grad_loss) {
   const int64_t blocks = a.n * a.parts;
   if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
-  CAMERA_BY_TYPE(dtype, hipLaunchKernelGGL((distill_grad_kernel<T>), launch_grid(blocks), dim3(kThreads), 0, stream, a, teacher, tail,
-                                           grad_loss));
+  CAMERA_BY_TYPE(dtype, a.threads, hipLaunchKernelGGL((distill_grad_kernel<T, TH>), launch_grid(blocks), dim3(TH), 0, stream, a, teacher,
+                                                      tail, grad_loss));
   return hipGetLastError();
 }
 

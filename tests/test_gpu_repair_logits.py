@@ -145,6 +145,26 @@ def test_logprobs_masks_and_ties(cam, vocab, dtype):
         check_logprobs(cam, z[i:i + 1], targets[i:i + 1], k, 1.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab,top_k", [(1, 1), (5, 5), (63, 63), (500, 64), (513, 64), (4097, 20), (16384, 64), (16384, 65), (16385, 64)])
+def test_many_short_rows(cam, vocab, top_k, dtype):
+    """1030 rows in short workgroups (and just beyond where they are used): rows with ties, masks and nothing left among ordinary ones."""
+    n = 1030
+    z = make_logits(n, vocab, dtype, 13, pad=3)
+    z[::7] = -math.inf
+    z[::7, vocab // 2:vocab // 2 + 9] = 1.0
+    z[3::7] = 0.25
+    z[5::7] = torch.finfo(TYPES[dtype]).min
+    z[5::7, vocab // 3] = -2.0
+    z[6::7] = torch.linspace(-4, 4, vocab, device="cuda").to(TYPES[dtype])
+    z[1024] = -math.inf
+    out = cam.token_logprobs(z, random_targets(n, vocab, 3), top_k=top_k)
+    rest = torch.arange(n, device="cuda") != 1024
+    check_logprobs(cam, z[rest], random_targets(n, vocab, 3)[rest], top_k, 1.0)
+    torch.cuda.synchronize()
+    assert torch.equal(out["top_idx"], top64(z, top_k)) and out["entropy"][1024] == 0
+
+
 def test_logprobs_do_not_depend_on_the_cut(cam):
     """One row by itself is cut into many parts, among many rows into few: the same tokens, and sums equal to their rounding."""
     logits = make_logits(2048, 9001, "bf16", 1)
@@ -353,7 +373,7 @@ def check_distill(cam, logits, idx, val, temperature, tail, dtype, g=None, **kw)
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("n,vocab,k,pad,offset,temperature", [
     (1, 1, 1, 0, 0, 1.0), (2, 7, 3, 1, 1, 1.0), (3, 7, 7, 0, 0, 2.0), (2, 5, 9, 0, 0, 1.0), (4, 4097, 64, 0, 3, 1.0),
-    (1, 50021, 256, 0, 0, 0.5), (65, 9001, 20, 3, 0, 2.0), (2049, 1500, 5, 0, 0, 1.0), (3, 151936, 100, 0, 0, 1.0), (2, 300001, 30, 0, 0, 1.0)])
+    (1, 50021, 256, 0, 0, 0.5), (65, 9001, 20, 3, 0, 2.0), (2049, 1500, 5, 0, 0, 1.0), (1024, 16384, 256, 0, 1, 1.0), (1024, 300, 256, 0, 0, 1.0), (1100, 16385, 7, 0, 0, 1.0), (3, 151936, 100, 0, 0, 1.0), (2, 300001, 30, 0, 0, 1.0)])
 def test_distill_loss_and_gradient(cam, n, vocab, k, pad, offset, temperature, tail, dtype):
     idx, val = make_teacher(n, vocab, k, temperature, 21, tail)
     logits = make_logits(n, vocab, dtype, 22 + vocab, pad, offset)
