@@ -93,7 +93,7 @@ struct GemmEpilogue {
   // kGated, kRounded, kPart: n_experts groups of group_rows left rows, one behind the other, cut as a GroupPlan says; of the
   // bucket tables only `zeros` is read
   int group_rows = 0;
-  bool small_tiles = false;
+  int small_tiles = 0;
 };
 hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int64_t ldx, int64_t d_model,
                                int64_t d_ff, int n_experts, const void* W_gate, const void* W_up,

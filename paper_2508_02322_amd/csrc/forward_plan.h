@@ -125,23 +125,24 @@ inline int64_t compact_product_workspace(int64_t pairs, int64_t experts, bool ti
 }
 
 // ---- products of plain groups of rows (the gated block and its gradients) ------------------------------------------------
-// bf16: tiles of 256 x 128 x 2, one workgroup a compute unit, or where they are few small ones of 64 x 64 x 2, up to three a
-// unit; float32: 64 x 32 x 2, up to six.
+// bf16: tiles of 256 x 128 x 2, one workgroup a compute unit, or where they are few small ones of 64 x 64 x 2, up to two a
+// unit or, with shallower rings, three; float32: 64 x 32 x 2, up to six.
 constexpr int kPlanSmallM = 64, kPlanSmallN = 64, kPlanF32M = 64, kPlanF32N = 32, kPlanF32K = 32;
 struct GroupPlan {
-  bool small = false;
+  int small = 0;         // 0 full-sized tiles, 1 small ones, 2 small ones with the shallower rings
   int parts = 1;         // of K
   int64_t m_tiles = 0;   // of all groups
   int64_t blocks = 0;    // workgroups of a launch in parts
 };
 // Time in ns of `here` workgroups on every die with k K tiles each: full-sized tiles in rounds as in split_ns; small ones, all at
-// once, by how many a unit has: 0.56, 0.69 and 0.82 us per K tile with one, two and three.  (More than that many small tiles draw the
+// once, by how many a unit has: 0.40, 0.54 and, in shallower rings, 0.82 us per K tile with one, two and three.  (More than that many small tiles draw the
 // chip's whole power and are slower than full-sized ones: dW of 8192 tokens, 2560 x 3584, 430 us in 2240 small tiles, 330 in 280.)
 inline int64_t group_ns(bool small, int64_t here, int64_t k) {
   const int64_t die_cus = kPlanCus / kPlanDies, on_unit = (here + die_cus - 1) / die_cus;
   if (!small) return on_unit * (1400 * k + 8000);
-  return on_unit > 3 ? INT64_MAX : (430 + 130 * on_unit) * k + 6000;
+  return on_unit > 3 ? INT64_MAX : (on_unit == 3 ? 820 : 260 + 140 * on_unit) * k + 6000;
 }
+inline int small_kind(int64_t here) { return here > 2 * (kPlanCus / kPlanDies) ? 2 : 1; }
 // most_parts: 1 where a product cannot be taken in parts.  A part's float32 rows (product_bytes) are written and read again at
 // 6 TB/s, in a launch more; they stay within the memory-side cache.
 inline GroupPlan group_plan(bool bf16, int64_t groups, int64_t rows, int64_t half_columns, int64_t k_ext, int most_parts) {
@@ -162,7 +163,7 @@ inline GroupPlan group_plan(bool bf16, int64_t groups, int64_t rows, int64_t hal
       int64_t& least = p > 1 ? best_parts_ns : best_ns;
       if (least < 0 || ns < least) {
         least = ns;
-        (p > 1 ? best_parts : best) = {small != 0, p, m_tiles, tiles_per_die(tiles) * p * kPlanDies};
+        (p > 1 ? best_parts : best) = {small ? small_kind(here) : 0, p, m_tiles, tiles_per_die(tiles) * p * kPlanDies};
       }
     }
   }

@@ -1571,8 +1571,12 @@ __global__ __launch_bounds__(256) void zero_hidden_kernel(const int32_t* __restr
 using Bf16Cfg = GemmCfg<2, 2, 4, 2, 64, 2, 3>;
 static_assert(Bf16Cfg::BM == kPlanTileM && Bf16Cfg::BN == kPlanTileN && Bf16Cfg::KT == kPlanTileK && kXcds == kPlanDies, "the plan's tile");
 
-// For products of few tiles: two waves of 32 x 64 x {gate, up}, three workgroups a compute unit.
-using SmallCfg = GemmCfg<2, 1, 1, 2, 64, 2, 2>;
+// For products of few tiles: two waves of 32 x 64 x {gate, up}.  With rings of three stages two workgroups fit a compute unit, with
+// two stages three.  A wave multiplies for 0.2 us per K tile and waits for its loads the rest of the time, so where one or two
+// workgroups a unit are all there are the deeper rings are faster (dX of 1021 tokens, 843 x 2048, 21 -> 15 us), and where there are
+// three to a unit having them all at once is (512 x 3584 x 2560 of 1024 tokens 57 us in two rounds, 47 in one).
+using SmallCfg = GemmCfg<2, 1, 1, 2, 64, 3, 3>;
+using SmallestCfg = GemmCfg<2, 1, 1, 2, 64, 2, 2>;
 
 // Whether the scalar-base form of the tile loads can address the operands: 32-bit byte offsets from the start of
 // the token matrix (a_rows rows of lda elements) and of one expert's weight matrix (b_rows rows of ldw elements).
@@ -1584,7 +1588,7 @@ bool fits_32bit_offsets(int64_t a_rows, int64_t lda, int64_t b_rows, int64_t ldw
 
 }  // namespace
 
-static_assert(SmallCfg::BM == kPlanSmallM && SmallCfg::BN == kPlanSmallN && F32_BM == kPlanF32M && F32_BN == kPlanF32N && F32_KT == kPlanF32K, "the plan's tiles");
+static_assert(SmallestCfg::BM == kPlanSmallM && SmallestCfg::BN == kPlanSmallN && SmallCfg::BM == kPlanSmallM && SmallCfg::BN == kPlanSmallN && F32_BM == kPlanF32M && F32_BN == kPlanF32N && F32_KT == kPlanF32K, "the plan's tiles");
 
 int gemm_tile_m(int dtype, int64_t d_ff) {
   (void)d_ff;
@@ -1619,6 +1623,12 @@ static hipError_t launch_bf16(hipStream_t stream, const void* X, int64_t ldx, in
   return hipGetLastError();
 }
 
+// GemmEpilogue.small_tiles: 0 full-sized tiles, 1 small ones, 2 small ones with the shallower rings
+template <int EPI, class... ARGS>
+static hipError_t launch_tiles(int small, ARGS... args) {
+  return small == 0 ? launch_bf16<EPI>(args...) : small == 1 ? launch_bf16<EPI, SmallCfg>(args...) : launch_bf16<EPI, SmallestCfg>(args...);
+}
+
 hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int64_t ldx, int64_t d_model,
                                int64_t d_ff, int n_experts, const void* W_gate, const void* W_up,
                                int64_t stride_gu, int max_tiles, const BucketTables& t, const GemmEpilogue& e) {
@@ -1639,14 +1649,11 @@ hipError_t launch_grouped_gemm(hipStream_t stream, int dtype, const void* X, int
       case GemmEpilogue::kProduct:
         return launch_bf16<kEpiProduct>(stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kGated:
-        return (e.small_tiles ? launch_bf16<kEpiGated, SmallCfg> : launch_bf16<kEpiGated>)(stream, X, ldx, d_model, d_ff, n_experts, W_gate,
-                                                                                          W_up, stride_gu, max_tiles, t, ep);
+        return launch_tiles<kEpiGated>(e.small_tiles, stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kRounded:
-        return (e.small_tiles ? launch_bf16<kEpiRounded, SmallCfg> : launch_bf16<kEpiRounded>)(stream, X, ldx, d_model, d_ff, n_experts,
-                                                                                               W_gate, W_up, stride_gu, max_tiles, t, ep);
+        return launch_tiles<kEpiRounded>(e.small_tiles, stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       case GemmEpilogue::kPart:
-        return (e.small_tiles ? launch_bf16<kEpiPart, SmallCfg> : launch_bf16<kEpiPart>)(stream, X, ldx, d_model, d_ff, n_experts, W_gate,
-                                                                                         W_up, stride_gu, max_tiles, t, ep);
+        return launch_tiles<kEpiPart>(e.small_tiles, stream, X, ldx, d_model, d_ff, n_experts, W_gate, W_up, stride_gu, max_tiles, t, ep);
       default:
         return hipErrorInvalidValue;
     }

@@ -89,7 +89,7 @@ def test_bf16_block(cam, n, d, f):
 
 
 # How dX is computed: tiles, and whether K is in parts.
-FORMS = {(40, 128, 5000, "bf16"): ("small", True), (700, 256, 200, "bf16"): ("small", False), (4096, 2048, 200, "bf16"): ("full", False),
+FORMS = {(40, 128, 5000, "bf16"): ("small", True), (700, 256, 200, "bf16"): ("small", False), (2500, 2048, 300, "bf16"): ("smallest", False), (4096, 2048, 200, "bf16"): ("full", False),
          (2048, 3584, 4000, "bf16"): ("full", True), (300, 772, 517, "f32"): ("full", True), (300, 772, 40, "f32"): ("full", False)}
 
 

@@ -55,7 +55,8 @@ def test_every_tile_has_a_workgroup(plan, bf16, groups):
                     part = groups * rows * 2 * half * 4
                     assert p["parts"] * part <= plan.bytes(part) <= 256 << 20 and up(k, 64 if bf16 else 32) >= 8 * p["parts"]
                 if p["small"]:
-                    assert up(tiles, 8) * p["parts"] <= 3 * 32
+                    here = up(tiles, 8) * p["parts"]
+                    assert here <= 3 * 32 and p["small"] == (1 if here <= 2 * 32 else 2)
                 assert plan(bf16, groups, rows, half, k, 1)["parts"] == 1
 
 
@@ -69,4 +70,4 @@ def test_the_gpu_tests_reach_every_form(plan):
     from tests.test_gpu_repair_block import FORMS
     for (n, d, f, dtype), form in FORMS.items():
         p = plan(dtype == "bf16", 1, n, d // 2, 2 * up(f, 64) * 64)     # dX
-        assert ("small" if p["small"] else "full", p["parts"] > 1) == form, (n, d, f, p)
+        assert (("full", "small", "smallest")[p["small"]], p["parts"] > 1) == form, (n, d, f, p)
