@@ -135,8 +135,10 @@ struct GroupPlan {
   int64_t blocks = 0;    // workgroups of a launch in parts
 };
 // Time in ns of `here` workgroups on every die with k K tiles each: full-sized tiles in rounds as in split_ns; small ones, all at
-// once, by how many a unit has: 0.40, 0.54 and, in shallower rings, 0.82 us per K tile with one, two and three.  (More than that many small tiles draw the
-// chip's whole power and are slower than full-sized ones: dW of 8192 tokens, 2560 x 3584, 430 us in 2240 small tiles, 330 in 280.)
+// once, by how many a unit has: 0.40, 0.54 and, in shallower rings, 0.82 us per K tile with one, two and three.  (More than that
+// many small tiles draw the chip's whole power and are slower than full-sized ones: dW of 8192 tokens, 2560 x 3584, 430 us in 2240
+// small tiles, 330 in 280.)  us, full-sized / small / as taken: dX of 64 tokens, 20480 x 3584, 666 in small tiles, 224 in eight parts;
+// of 1024 tokens 765 / 442; forward of 1024 tokens, 2560 x 3584, 80 tiles of 56 K tiles or 640 small ones: 86 by the rule above / 46.
 inline int64_t group_ns(bool small, int64_t here, int64_t k) {
   const int64_t die_cus = kPlanCus / kPlanDies, on_unit = (here + die_cus - 1) / die_cus;
   if (!small) return on_unit * (1400 * k + 8000);

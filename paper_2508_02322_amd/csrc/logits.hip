@@ -386,11 +386,25 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
         else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
       });
       __syncthreads();
-      if (tid == 0) {
-        int digit = 255;
-        for (; digit > 0 && want > sm.hist[digit]; --digit) want -= sm.hist[digit];
-        sm.prefix = prefix | (uint64_t)digit << shift;
-        sm.want = want;
+      if (tid < kWave) {  // the digit at which the counts from 255 down reach `want`: lane l has four, from 255 - 4 l down
+        int count[4], mine = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine += count[i] = sm.hist[255 - 4 * tid - i];
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+          const int more = __shfl_up(upto, d);
+          if (tid >= d) upto += more;
+        }
+        int left = want - (upto - mine);  // still to be found among this lane's four
+        if (left > 0 && left <= mine) {   // one lane
+          int i = 0;
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (i == j && left > count[j]) left -= count[j], i = j + 1;
+          sm.prefix = prefix | (uint64_t)(255 - 4 * tid - i) << shift;
+          sm.want = left;
+        }
       }
       __syncthreads();
       prefix = sm.prefix;
