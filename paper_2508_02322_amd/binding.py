@@ -132,7 +132,7 @@ def _check_flat(t, name: str, dtype=None, device=None):
 
 def _row_stride(t) -> int:
     """Elements between rows; a matrix of at most one row has none of its own (torch leaves any value there)."""
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    return t.shape[1] if t.shape[0] <= 1 else t.stride(0)
 
 
 # The current stream's handle by itself where torch has it: a Stream object around it takes 2 us, a sixth of a small call.
@@ -496,14 +496,18 @@ class Camera:
         self._check_gated(X, W_gate, W_up)
         n, d_ff = X.shape[0], W_gate.shape[0]
         v = 16 // X.element_size()
+        whole = (d_ff + v - 1) // v * v
         if H is None:
-            H = torch.empty((n, (d_ff + v - 1) // v * v), dtype=X.dtype, device=self.device)[:, :d_ff]
-        _check_matrix(H, "H", like=X)
-        _require(tuple(H.shape) == (n, d_ff), "H: must be [n, d_ff]")
+            H = torch.empty((n, whole), dtype=X.dtype, device=self.device)[:, :d_ff]
+        else:
+            _check_matrix(H, "H", like=X)
+            _require(tuple(H.shape) == (n, d_ff), "H: must be [n, d_ff]")
+            end = H.storage_offset() + (n - 1) * H.stride(0) + whole
+            _require(n == 0 or end * H.element_size() <= H.untyped_storage().nbytes(), "H: its last row ends inside a 16-byte vector")
         pre = torch.empty((n, 2, (d_ff + 7) // 8 * 8), dtype=torch.float32, device=self.device) if want_pre else None
         self._check(self.lib.camera_gated_ffn(
             self._ctx, _stream_handle(self.device), _ptr(X), _dtype_code(X), n, X.shape[1], _row_stride(X), _ptr(W_gate), _ptr(W_up),
-            d_ff, _ptr(H), _row_stride(H), _ptr(pre)))
+            d_ff, _ptr(H), max(H.stride(0), d_ff), _ptr(pre)))
         return (H, pre) if want_pre else H
 
     def gated_ffn_backward(self, X, W_gate, W_up, dH, pre=None, want=(True, True, True)):

@@ -244,3 +244,20 @@ def test_binding_refuses_what_the_library_cannot_see(cam):
                  lambda: cam.gated_ffn(X.cpu(), Wg.cpu(), Wu.cpu()), lambda: cam.gated_ffn_backward(X, Wg, Wu, dH[:, :20]), lambda: cam.gated_ffn_backward(X, Wg, Wu, dH, pre=dH.float())):
         with pytest.raises(binding.CameraError):
             call()
+    short = torch.empty(3 * 32 + 20, dtype=X.dtype, device="cuda")          # the last row's zeros would lie behind the buffer
+    with pytest.raises(binding.CameraError, match="last row"):
+        cam.gated_ffn(X, Wg[:20].contiguous(), Wu[:20].contiguous(), H=short.as_strided((4, 20), (32, 1)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_row_has_no_stride(cam, dtype):
+    """torch leaves any number as the row stride of a single row, here an odd one and one of 0; only the address counts."""
+    X, Wg, Wu, dH = make(1, 64, 24, dtype, 3)
+    H, pre = cam.gated_ffn(X, Wg, Wu, want_pre=True)
+    want = cam.gated_ffn_backward(X, Wg, Wu, dH, pre=pre)
+    for stride in (0, 1, 67):
+        x, dh = X.as_strided((1, 64), (stride, 1)), dH.as_strided((1, 24), (stride, 1))
+        assert x.stride(0) == stride
+        assert torch.equal(cam.gated_ffn(x, Wg, Wu), H)
+        for a, b in zip(cam.gated_ffn_backward(x, Wg, Wu, dh, pre=pre), want):
+            assert torch.equal(a, b)
