@@ -260,7 +260,7 @@ struct SelectSmem {
   int32_t chosen[kChosen];         // cells that may hold candidates: cell * TH + stripe
   uint64_t keys[kCandidates];
   int32_t hist[256];
-  uint32_t bound;
+  uint32_t bound, least, most;
   int32_t n_chosen, n_keys;
   uint64_t prefix;
   int32_t want;
@@ -311,8 +311,10 @@ struct ListKeys {
 // its lower 16 bits left 0 (all that a bf16 value has; counting for every maximum how many are larger took the workgroup 7 us).
 // The values not below it lie in the cells whose maximum is not, mostly k of them, which are read again, from the caches.  The
 // keys are all different, so the order in which candidates are found does not show.  Where more values reach the bound than there
-// is room for (ties: a constant row, a mask by the type's lowest value), the k-th largest key is found by its digits, eight passes
-// over the source.  4096 x 151936 bf16, us: 237 without alternatives, 228 to 231 with up to 64, 281 with 256 (half the lines again).
+// is room for, they are mostly equal (a mask by the type's lowest value with fewer tokens left than wanted, a constant row): then
+// the larger values are taken and of the equal ones the first, in index order, one pass and the beginning of another.  Otherwise
+// the k-th largest key is found by its digits, eight passes over the source.  1024 x 102400 bf16, 5 tokens left, 20 alternatives: 101 us,
+// 745 by digits, 42 without ties.  4096 x 151936 bf16, us: 237 without alternatives, 228 to 231 with up to 64, 281 with 256 (half the lines again).
 template <int TH, class SOURCE, class OUT>
 __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem<TH>& sm, OUT&& out) {
   constexpr int kWaves = TH / kWave, kCandidates = SelectSmem<TH>::kCandidates, kChosen = SelectSmem<TH>::kChosen;
@@ -364,28 +366,45 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
   }
   int n_keys = sm.n_keys;
   if (n_chosen > kChosen || n_keys > kCandidates) {
-    auto every = [&](auto&& f) {
+    // Step 8: the larger keys, and the range of the values that share the bound's upper half.  Steps 7 to 0: a digit.  Then: the keys.
+    uint64_t prefix = 0;
+    int want = k;
+    bool equal = false;
+    for (int step = 8; step >= -1 && !equal; --step) {
+      __syncthreads();
+      for (int i = tid; i < 256; i += TH) sm.hist[i] = 0;
+      if (tid == 0) {
+        sm.n_keys = 0;
+        sm.least = 0xffffffffu;
+        sm.most = 0;
+      }
+      __syncthreads();
+      uint32_t least = 0xffffffffu, most = 0;
       for (int c = 0; c < cells; ++c)
         for (int pos = 0; pos < positions; ++pos)
           src.at(tid, c, pos, [&](uint32_t bits, int index) {
-            if (bits >= bound && bits != 0) f(make_key(bits, index));
+            if (bits < bound || bits == 0) return;
+            const uint64_t key = make_key(bits, index);
+            if (step == 8 && bits >> 16 == bound >> 16) {
+              least = min(least, bits);
+              most = max(most, bits);
+            } else if (step == 8 || step < 0) {
+              if (key >= prefix) add_key(key);
+            } else if (step == 7 || (key ^ prefix) >> (8 * step + 8) == 0) {
+              // lanes that count the same digit as the first one add once
+              const int digit = (int)(key >> 8 * step & 255), lead = __builtin_amdgcn_readfirstlane(digit);
+              const uint64_t same = __ballot(digit == lead);
+              if (digit != lead) atomicAdd(&sm.hist[digit], 1);
+              else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
+            }
           });
-    };
-    uint64_t prefix = 0;
-    int want = k;
-    for (int shift = 56; shift >= 0; shift -= 8) {
+      if (most != 0) {
+        atomicMin(&sm.least, least);
+        atomicMax(&sm.most, most);
+      }
       __syncthreads();
-      for (int i = tid; i < 256; i += TH) sm.hist[i] = 0;
-      __syncthreads();
-      every([&](uint64_t key) {
-        if (shift < 56 && (key ^ prefix) >> (shift + 8) != 0) return;
-        // lanes that count the same digit as the first one add once
-        const int digit = (int)(key >> shift & 255), lead = __builtin_amdgcn_readfirstlane(digit);
-        const uint64_t same = __ballot(digit == lead);
-        if (digit != lead) atomicAdd(&sm.hist[digit], 1);
-        else if (tid % kWave == __ffsll((unsigned long long)same) - 1) atomicAdd(&sm.hist[digit], (int)__popcll(same));
-      });
-      __syncthreads();
+      if (step == 8) equal = sm.n_keys < k && sm.least == sm.most;
+      if (step == 8 || step < 0) continue;
       if (tid < kWave) {  // the digit at which the counts from 255 down reach `want`: lane l has four, from 255 - 4 l down
         int count[4], mine = 0;
 #pragma unroll
@@ -402,7 +421,7 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
 #pragma unroll
           for (int j = 0; j < 3; ++j)
             if (i == j && left > count[j]) left -= count[j], i = j + 1;
-          sm.prefix = prefix | (uint64_t)(255 - 4 * tid - i) << shift;
+          sm.prefix = prefix | (uint64_t)(255 - 4 * tid - i) << 8 * step;
           sm.want = left;
         }
       }
@@ -410,13 +429,42 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
       prefix = sm.prefix;
       want = sm.want;
     }
-    if (tid == 0) sm.n_keys = 0;
-    __syncthreads();
-    every([&](uint64_t key) {
-      if (key >= prefix) add_key(key);
-    });
-    __syncthreads();
-    n_keys = sm.n_keys;  // k, or as many as there are
+    n_keys = sm.n_keys;  // k, or the ones larger than the equal values
+    if (equal) {
+      // every round of the source is in index order over the threads (of a list: the equal values' order in it is the index order)
+      const uint32_t value = sm.most;
+      for (int c = 0; c < cells && n_keys < k; ++c)
+        for (int pos = 0; pos < positions && n_keys < k; ++pos) {
+          uint32_t found = 0;  // a bit per element, the last one's the lowest
+          int last = 0;
+          src.at(tid, c, pos, [&](uint32_t bits, int index) {
+            found = found << 1 | (bits == value);
+            last = index;
+          });
+          const int mine = __popc(found);
+          int upto = mine;
+#pragma unroll
+          for (int d = 1; d < kWave; d <<= 1) {
+            const int more = __shfl_up(upto, d);
+            if (tid % kWave >= d) upto += more;
+          }
+          __syncthreads();  // the previous round's totals have been read
+          if (tid % kWave == kWave - 1) sm.hist[tid / kWave] = upto;
+          __syncthreads();
+          int place = n_keys + upto - mine;
+          for (int w = 0; w < kWaves; ++w) {
+            n_keys += sm.hist[w];
+            place += w < tid / kWave ? sm.hist[w] : 0;
+          }
+          for (; found != 0 && place < k; ++place) {
+            const int back = 31 - __clz(found);
+            sm.keys[place] = make_key(value, last - back);
+            found ^= 1u << back;
+          }
+        }
+      n_keys = min(n_keys, k);
+      __syncthreads();
+    }
   }
   if (n_keys <= kCounted) {
     if (tid < n_keys) {
@@ -474,8 +522,10 @@ __device__ __forceinline__ void write_alternative(const LogprobArgs& a, const Ru
       none ? -INFINITY : (of_order_bits((uint32_t)(key >> 32)) - r.m) * a.inv_temperature - log_sum;
 }
 
-// A workgroup has a part of a row; with one part a row it ends it, else it leaves its sums and its alternatives' keys.
-template <class T, int TH, bool TOP>
+// A workgroup has a part of a row; where that is the WHOLE row it ends it, else it leaves its sums and its alternatives' keys.  Four
+// workgroups share a compute unit only with at most 64 vector and 80 scalar registers a wave: with both ends in one kernel (87 scalar
+// ones) three did, and 64 x 102400 bf16 took 15.1 us where it takes 11.7.
+template <class T, int TH, bool TOP, bool WHOLE>
 __global__ __launch_bounds__(TH, 4) void logprobs_kernel(LogprobArgs a) {
   __shared__ Slots slots;
   const int64_t block = linear_block();
@@ -492,12 +542,12 @@ __global__ __launch_bounds__(TH, 4) void logprobs_kernel(LogprobArgs a) {
   }
   const Running mine = stream_part<true, false, TOP>(p, scale, nullptr, TOP ? select->cell_max : nullptr, [] {});
   const Running r = block_running<TH>(mine, scale, slots);
-  if (a.parts == 1) finish_logprobs<T>(r, a, row);
+  if constexpr (WHOLE) finish_logprobs<T>(r, a, row);
   else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
   if constexpr (TOP) {
     const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
     select_top<TH>(LogitKeys<T, TH>{p}, order_bits(mine.m), a.top_k, *select, [&](int place, uint64_t key) {
-      if (a.parts == 1) write_alternative(a, r, log_sum, row, place, key);
+      if constexpr (WHOLE) write_alternative(a, r, log_sum, row, place, key);
       else a.part_keys[block * a.top_k + place] = key;
     });
   }
@@ -921,11 +971,17 @@ hipError_t launch_token_logprobs(hipStream_t stream, int dtype, const LogprobArg
   if (blocks <= 0 || blocks >= (int64_t(1) << 31)) return hipErrorInvalidValue;
   if (a.threads == kShort ? a.parts != 1 || a.top_k > kShortTop : a.threads != kLong) return hipErrorInvalidValue;
   CAMERA_BY_TYPE(dtype, a.threads, {
-    if (a.top_k > 0) hipLaunchKernelGGL((logprobs_kernel<T, TH, true>), launch_grid(blocks), dim3(TH), 0, stream, a);
-    else hipLaunchKernelGGL((logprobs_kernel<T, TH, false>), launch_grid(blocks), dim3(TH), 0, stream, a);
-    if (a.parts > 1) {
-      if (a.top_k > 0) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), launch_grid(a.n), dim3(kLong), 0, stream, a);
-      else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), launch_grid(a.n), dim3(kLong), 0, stream, a);
+    if (a.parts == 1) {
+      if (a.top_k > 0) hipLaunchKernelGGL((logprobs_kernel<T, TH, true, true>), launch_grid(blocks), dim3(TH), 0, stream, a);
+      else hipLaunchKernelGGL((logprobs_kernel<T, TH, false, true>), launch_grid(blocks), dim3(TH), 0, stream, a);
+    } else if constexpr (TH == kLong) {
+      if (a.top_k > 0) {
+        hipLaunchKernelGGL((logprobs_kernel<T, TH, true, false>), launch_grid(blocks), dim3(TH), 0, stream, a);
+        hipLaunchKernelGGL((logprobs_join_kernel<T, true>), launch_grid(a.n), dim3(TH), 0, stream, a);
+      } else {
+        hipLaunchKernelGGL((logprobs_kernel<T, TH, false, false>), launch_grid(blocks), dim3(TH), 0, stream, a);
+        hipLaunchKernelGGL((logprobs_join_kernel<T, false>), launch_grid(a.n), dim3(TH), 0, stream, a);
+      }
     }
   });
   return hipGetLastError();

@@ -146,6 +146,30 @@ def test_logprobs_masks_and_ties(cam, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 1024])
+def test_more_candidates_than_room(cam, n, dtype):
+    """Thousands of values reach the bound: all equal; equal but for a few larger ones, behind and among them; different in their last
+    bits only; larger ones in a few stripes, more of them than wanted; equal ones that begin late; the same with every second ruled out."""
+    vocab, vec = (16000, 8 if dtype == "bf16" else 4)
+    at = torch.arange(vocab, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    noise = torch.rand(vocab, generator=g, device="cuda")
+    rows = [torch.ones(vocab, device="cuda"), 1.0 + 1e-3 * noise,
+            torch.where(at % 3001 == 7, 3.0 + at / vocab, torch.full_like(noise, 0.5)),
+            torch.where((at // vec) % 128 < 5, 2.0 + noise, torch.full_like(noise, 0.5)),
+            torch.where((at // vec) % 512 < 10, 2.0 + noise, torch.full_like(noise, 0.5)),
+            torch.where(at > 9000, 1.0, -1.0), torch.where(at % 2 == 0, -math.inf, 0.25), torch.where(noise < 0.5, 0.25, 0.25 + 2.0 ** -24)]
+    z = torch.stack(rows).to(TYPES[dtype])
+    if n > len(rows):
+        z = z.repeat(n // len(rows), 1)
+    for k in (1, 20, 64, 256):
+        for part in ([z] if n > 1 else [z[i:i + 1] for i in range(len(rows))]):
+            out = cam.token_logprobs(part, top_k=k)
+            torch.cuda.synchronize()
+            assert torch.equal(out["top_idx"], top64(part, k)), (n, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("vocab,top_k", [(1, 1), (5, 5), (63, 63), (500, 64), (513, 64), (4097, 20), (16384, 64), (16384, 65), (16385, 64)])
 def test_many_short_rows(cam, vocab, top_k, dtype):
     """1030 rows in short workgroups (and just beyond where they are used): rows with ties, masks and nothing left among ordinary ones."""
@@ -495,6 +519,31 @@ def test_logit_calls_on_another_stream_and_in_a_graph(cam):
         for a, b in zip(kept, step()):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+def test_two_graphs_on_one_workspace(cam):
+    """Two captured calls that cut their rows share the context's workspace: replayed in turn, each gives its own result."""
+    def capture(n, vocab, k, seed):
+        z = make_logits(n, vocab, "bf16", seed)
+        cam.token_logprobs(z, top_k=k)
+        torch.cuda.synchronize()
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.stream(stream):
+            with torch.cuda.graph(graph, stream=stream):
+                out = cam.token_logprobs(z, top_k=k)
+        torch.cuda.synchronize()
+        return z, k, graph, out
+    cam.token_logprobs(make_logits(2, 9000, "bf16", 1), top_k=40)      # the workspace has its size before the first capture
+    both = [capture(2, 50000, 40, 1), capture(5, 30001, 17, 2)]
+    for trial in range(3):
+        for z, k, graph, out in both:
+            graph.replay()
+        torch.cuda.synchronize()
+        for z, k, graph, out in both:
+            assert torch.equal(out["top_idx"], top64(z, k))
+            for key, want in cam.token_logprobs(z, top_k=k).items():
+                assert torch.equal(out[key], want), key
+            z.copy_(-z)
 
 
 def test_rows_beyond_32_bit_offsets(cam):
