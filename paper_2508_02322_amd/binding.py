@@ -452,7 +452,7 @@ class Camera:
         tail: the tokens that the teacher does not list are one more class (teacher_logprob taken at this temperature); else the
         teacher's distribution is renormalised over the listed ones.  Returns dict(loss [n], stats [n, 5])."""
         n = logits.shape[0]
-        k = teacher_idx.shape[1]
+        k = teacher_idx.shape[-1]
         self._check_logits(logits, [(teacher_idx, "teacher_idx", torch.int32, (n, k)),
                                     (teacher_logprob, "teacher_logprob", torch.float32, (n, k))])
         out = {"loss": torch.empty(n, dtype=torch.float32, device=self.device),
@@ -468,7 +468,7 @@ class Camera:
         """Gradient with respect to the logits of sum(grad_loss * loss); stats as distill_topk left them, the other arguments as it
         had them.  dlogits: written there (accumulate: added to it); it may be `logits` itself."""
         n = logits.shape[0]
-        k = teacher_idx.shape[1]
+        k = teacher_idx.shape[-1]
         self._check_logits(logits, [(teacher_idx, "teacher_idx", torch.int32, (n, k)),
                                     (teacher_logprob, "teacher_logprob", torch.float32, (n, k)),
                                     (stats, "stats", torch.float32, (n, DISTILL_STATS)), (grad_loss, "grad_loss", torch.float32, (n,))])

@@ -186,7 +186,10 @@ def recovery_step(cam, logits, targets, teacher: Teacher, grad_logprob, grad_kl,
     """One step of repairing a pruned model: the log probabilities of the targets (at temperature 1), the divergence from the
     teacher (at the teacher's temperature; tail: its unlisted tokens as one class), and the gradient with respect to the logits of
     sum(grad_logprob * logprob) + sum(grad_kl * kl).  For a mean over n positions with weight w on the teacher: grad_logprob =
-    -(1 - w) / n, grad_kl = w / n (times the temperature squared, if its gradient is to keep its size)."""
+    -(1 - w) / n, grad_kl = w / n (times the temperature squared, if its gradient is to keep its size).  dlogits may not be `logits`:
+    both gradients read them."""
+    if dlogits is not None and dlogits.data_ptr() == logits.data_ptr() and logits.numel() > 0:
+        raise ValueError("dlogits: may not be logits, which the second gradient reads behind the first")
     lp = cam.token_logprobs(logits, targets)
     kd = cam.distill_topk(logits, teacher.idx, teacher.logprob, temperature=teacher.temperature, tail=tail)
     dlogits = cam.token_logprobs_backward(logits, targets, lp["stats"], grad_logprob, dlogits=dlogits)

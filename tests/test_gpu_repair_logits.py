@@ -584,3 +584,7 @@ def test_binding_refuses_what_the_library_cannot_see(cam):
                  lambda: cam.token_logprobs(z, top_k=101), lambda: cam.token_logprobs(z, temperature=0.0)):
         with pytest.raises(binding.CameraError):
             call()
+    for call in (lambda: cam.distill_topk(z, idx[:, 0], val[:, 0]),
+                 lambda: cam.distill_topk_backward(z, idx[:, 0], val[:, 0], torch.zeros((4, 5), device="cuda"), torch.zeros(4, device="cuda"))):
+        with pytest.raises(binding.CameraError, match="teacher_idx"):
+            call()

@@ -101,6 +101,18 @@ def test_recovery_step(cam, dtype):
     assert bool((err <= tol).all()), float((err / tol).max())
 
 
+def test_recovery_step_refuses_its_logits_as_the_gradient(cam):
+    """Refused before anything is written: the first gradient would replace what the second one reads."""
+    logits = torch.randn((3, 64), device="cuda")
+    before = logits.clone()
+    teacher = pipeline.teacher_of(cam, logits, 4)
+    g = torch.ones(3, device="cuda")
+    with pytest.raises(ValueError, match="dlogits"):
+        pipeline.recovery_step(cam, logits, torch.zeros(3, dtype=torch.int32, device="cuda"), teacher, g, g, dlogits=logits)
+    torch.cuda.synchronize()
+    assert torch.equal(logits, before)
+
+
 def test_recovery_through_the_block(cam):
     """Logits = (block of the pruned shared expert) W_down^T W_head^T; the gradients of the kept rows and of the tokens against autograd
     in float64.  dH reaches the block in bf16 (half a step), the block rounds dG, dU and its results: with independent
