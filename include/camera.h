@@ -428,7 +428,8 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
  * are known (top_idx and top_logprob of camera_token_logprobs on its logits): the Kullback-Leibler divergence
  *   loss[i] = sum over the listed tokens j of q_j (log q_j - log p_j)
  * with p = softmax(logits / temperature) over the whole vocabulary and q the teacher's distribution:
- *   flags 0                    q = softmax(teacher_logprob / temperature) over the row's entries (logits do as well there)
+ *   flags 0                    q = softmax(teacher_logprob / temperature) over the row's entries: logits, or log probabilities at
+ *            temperature 1 (those taken at this temperature, as CAMERA_DISTILL_TAIL wants them, times the temperature do as well)
  *   flags CAMERA_DISTILL_TAIL  q_j = exp(teacher_logprob_j), which were taken at this temperature, and all tokens that are not
  *            listed are one more class: + q_r (log q_r - log p_r), q_r = max(0, 1 - sum q_j), p_r = the sum of their p.  Where no
  *            token is left for it the class drops out.

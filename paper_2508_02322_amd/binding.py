@@ -450,7 +450,8 @@ class Camera:
         """Kullback-Leibler divergence of softmax(logits / temperature) from a teacher of which the most likely tokens are known:
         teacher_idx int32 [n, k], teacher_logprob [n, k] (top_idx and top_logprob of token_logprobs on the teacher's logits).
         tail: the tokens that the teacher does not list are one more class (teacher_logprob taken at this temperature); else the
-        teacher's distribution is renormalised over the listed ones.  Returns dict(loss [n], stats [n, 5])."""
+        teacher's distribution is softmax(teacher_logprob / temperature) over the listed ones: logits, or log probabilities at temperature
+        1, since here they are divided by the temperature.  Returns dict(loss [n], stats [n, 5])."""
         n = logits.shape[0]
         k = teacher_idx.shape[-1]
         self._check_logits(logits, [(teacher_idx, "teacher_idx", torch.int32, (n, k)),

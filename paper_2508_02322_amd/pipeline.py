@@ -184,15 +184,18 @@ class RecoveryStep:
 
 def recovery_step(cam, logits, targets, teacher: Teacher, grad_logprob, grad_kl, tail: bool = True, dlogits=None) -> RecoveryStep:
     """One step of repairing a pruned model: the log probabilities of the targets (at temperature 1), the divergence from the
-    teacher (at the teacher's temperature; tail: its unlisted tokens as one class), and the gradient with respect to the logits of
-    sum(grad_logprob * logprob) + sum(grad_kl * kl).  For a mean over n positions with weight w on the teacher: grad_logprob =
-    -(1 - w) / n, grad_kl = w / n (times the temperature squared, if its gradient is to keep its size).  dlogits may not be `logits`:
-    both gradients read them."""
+    teacher (at the teacher's temperature; tail: its unlisted tokens as one class, else the teacher renormalised over its
+    listed tokens), and the gradient with respect to the logits of sum(grad_logprob * logprob) + sum(grad_kl * kl).
+    For a mean over n positions with weight w on the teacher: grad_logprob = -(1 - w) / n, grad_kl = w / n (times the temperature
+    squared, if its gradient is to keep its size).  dlogits may not be `logits`: both gradients read them."""
     if dlogits is not None and dlogits.data_ptr() == logits.data_ptr() and logits.numel() > 0:
         raise ValueError("dlogits: may not be logits, which the second gradient reads behind the first")
     lp = cam.token_logprobs(logits, targets)
-    kd = cam.distill_topk(logits, teacher.idx, teacher.logprob, temperature=teacher.temperature, tail=tail)
+    # Without the unlisted class the call divides the teacher's values by the temperature itself, so they go to it as of temperature 1
+    # (but for a constant of the row, which its softmax does not see): one rounding, half a step, more.
+    teacher_logprob = teacher.logprob if tail or teacher.temperature == 1.0 else teacher.logprob * teacher.temperature
+    kd = cam.distill_topk(logits, teacher.idx, teacher_logprob, temperature=teacher.temperature, tail=tail)
     dlogits = cam.token_logprobs_backward(logits, targets, lp["stats"], grad_logprob, dlogits=dlogits)
-    cam.distill_topk_backward(logits, teacher.idx, teacher.logprob, kd["stats"], grad_kl, temperature=teacher.temperature, tail=tail,
+    cam.distill_topk_backward(logits, teacher.idx, teacher_logprob, kd["stats"], grad_kl, temperature=teacher.temperature, tail=tail,
                               dlogits=dlogits, accumulate=True)
     return RecoveryStep(lp["logprob"], lp["entropy"], kd["loss"], dlogits)
