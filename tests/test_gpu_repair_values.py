@@ -1,0 +1,155 @@
+"""Logits that no sum survives, and classes that are next to impossible: NaN is not hidden, and a gradient that the definition makes
+finite is finite and right."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+# rows in parts, whole in long workgroups, whole in short ones
+SHAPES = [(12, 9001), (1100, 17001), (1030, 3001)]
+
+
+def rows_of(n, vocab, dtype, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (3 * torch.randn((n, vocab), generator=gen, device="cuda")).to(TYPES[dtype])
+
+
+def spoil(z, idx):
+    """Rows 1 to 9: NaN at the target, at a listed token, elsewhere, at the last token; all NaN; NaN and ruled out tokens only; +Inf;
+    +Inf at a listed token; NaN and +Inf."""
+    nan, vocab = float("nan"), z.shape[1]
+    z = z.clone()
+    z[1, 0] = nan
+    z[2, idx[2, 3].long()] = nan
+    z[3, 777] = nan
+    z[4, vocab - 1] = nan
+    z[5] = nan
+    z[6] = -math.inf
+    z[6, vocab // 2] = nan
+    z[7, 2222] = math.inf
+    z[8, idx[8, 0].long()] = math.inf
+    z[9, 5] = nan
+    z[9, 6] = math.inf
+    return z
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_log_probabilities_show_nan(cam, n, vocab, dtype):
+    z = rows_of(n, vocab, dtype, 1)
+    targets = torch.zeros(n, dtype=torch.int32, device="cuda")
+    top = cam.token_logprobs(z, targets, top_k=10)
+    bad = spoil(z, top["top_idx"])
+    out, plain = cam.token_logprobs(bad, targets, top_k=10), cam.token_logprobs(bad, targets)
+    ones = torch.ones(n, device="cuda")
+    grad = cam.token_logprobs_backward(bad, targets, out["stats"], ones, out["entropy"], ones)
+    want = cam.token_logprobs_backward(z, targets, top["stats"], ones, top["entropy"], ones)
+    only = cam.token_logprobs_backward(bad, targets, out["stats"], ones)
+    torch.cuda.synchronize()
+    spoiled = torch.zeros(n, dtype=torch.bool, device="cuda")
+    spoiled[1:10] = True
+    for o in (out, plain):
+        for key in ("logprob", "entropy"):
+            assert torch.equal(o[key].isnan(), spoiled), key
+        assert torch.equal(o["stats"][:, 1].isnan(), spoiled)
+    for g in (grad, only):
+        assert bool(g[spoiled].isnan().all()) and not bool(g[~spoiled].isnan().any())
+    for key in top:
+        assert torch.equal(out[key][~spoiled], top[key][~spoiled]), key
+    assert torch.equal(grad[~spoiled], want[~spoiled])
+    assert bool(((out["top_idx"] >= -1) & (out["top_idx"] < vocab)).all())
+    # a row without gradient stays without one
+    none = cam.token_logprobs_backward(bad, targets, out["stats"], torch.zeros(n, device="cuda"))
+    torch.cuda.synchronize()
+    assert not bool(none.any())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_distillation_shows_nan(cam, n, vocab, tail, dtype):
+    z = rows_of(n, vocab, dtype, 2)
+    top = cam.token_logprobs(rows_of(n, vocab, dtype, 3), top_k=10)
+    teacher = top["top_idx"], top["top_logprob"]
+    bad = spoil(z, top["top_idx"])
+    ones = torch.ones(n, device="cuda")
+    good, out = cam.distill_topk(z, *teacher, tail=tail), cam.distill_topk(bad, *teacher, tail=tail)
+    want = cam.distill_topk_backward(z, *teacher, good["stats"], ones, tail=tail)
+    got = cam.distill_topk_backward(bad, *teacher, out["stats"], ones, tail=tail)
+    torch.cuda.synchronize()
+    spoiled = torch.zeros(n, dtype=torch.bool, device="cuda")
+    spoiled[1:10] = True
+    assert torch.equal(out["loss"].isnan(), spoiled)
+    assert bool(got[spoiled].isnan().all()) and not bool(got[~spoiled].isnan().any())
+    for key in good:
+        assert torch.equal(out[key][~spoiled], good[key][~spoiled]), key
+    assert torch.equal(got[~spoiled], want[~spoiled])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.0, 0.5, 2.0])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_unlisted_class_next_to_impossible(cam, n, vocab, T, dtype):
+    """The student keeps the listed tokens and gives all others a mask's value (rows: -50, -200, -1e3, -1e4, -1e9, the type's lowest,
+    the last two with a few tokens less ruled out), the teacher has a quarter of its probability there.  The unlisted tokens' gradient is
+    p - q_r softmax(unlisted): about -1 / (4 unlisted) each, whatever the mask.
+
+    Tolerance, relative to the two terms: L additions in each sum, 4 u per unit of the exponents that are taken, d from the class's largest
+    logit, w = log q_r - log sum exp d; where the class is within e^-256 its ratio to q_r goes through float32 as a logarithm, 4 u each unit."""
+    k = 8
+    z = rows_of(n, vocab, dtype, 4)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    idx = torch.stack([torch.randperm(vocab, generator=gen, device="cuda")[:k] for _ in range(8)]).repeat(-(-n // 8), 1)[:n].int()
+    lowest = torch.finfo(TYPES[dtype]).min
+    masks = [-50.0, -200.0, -1e3, -1e4, -1e9, lowest, -1e9, lowest]
+    listed = torch.zeros((n, vocab), dtype=torch.bool, device="cuda").scatter_(1, idx.long(), True)
+    some = torch.rand(vocab, generator=gen, device="cuda") < 0.3
+    noise = 2 * torch.rand((n, vocab), generator=gen, device="cuda")
+    for i, value in enumerate(masks):
+        fill = torch.full((vocab,), value, device="cuda")
+        if value > -1e5:
+            fill = fill - noise[i]                         # not all alike where the type can tell
+        elif i >= 6:
+            fill[some] = value / 2
+        z[i::8] = torch.where(listed[i::8], z[i::8], fill.to(TYPES[dtype]))
+    share = torch.rand((n, k), generator=gen, device="cuda") + 0.1
+    val = (0.75 * share / share.sum(1, keepdim=True)).log()
+    g = torch.linspace(0.5, 2.0, n, device="cuda")
+    out = cam.distill_topk(z, idx, val, temperature=T, tail=True)
+    got = cam.distill_topk_backward(z, idx, val, out["stats"], g, temperature=T, tail=True)
+    added = cam.distill_topk_backward(z, idx, val, out["stats"], g, temperature=T, tail=True, dlogits=torch.zeros_like(z), accumulate=True)
+    torch.cuda.synchronize()
+
+    d = z.double().masked_fill(listed, -math.inf)
+    m_r = d.amax(1, keepdim=True)
+    d = (d - m_r) / T
+    log_s = torch.logsumexp(d, 1, keepdim=True)
+    here = z.double().gather(1, idx.long()) / T
+    log_sum = torch.logaddexp(torch.logsumexp(here, 1, keepdim=True), m_r / T + log_s)
+    q = val.double().exp()
+    q_r = 1 - q.sum(1, keepdim=True)
+    log_rest = m_r / T + log_s - log_sum
+    loss = (q * (val.double() - (here - log_sum))).sum(1) + (q_r * (q_r.log() - log_rest))[:, 0]
+    L = vocab / 128 + 40
+    fits = loss < 3e38
+    assert bool(((out["loss"].double() - loss).abs()[fits] <= ((L + 32) * U + 4 * U * loss.abs())[fits]).all())
+    within = (d - log_s).exp()                              # of the class; 0 at the listed tokens
+    unlisted = within * log_rest.exp() - q_r * within
+    p = torch.zeros_like(unlisted).scatter_(1, idx.long(), (here - log_sum).exp())
+    dense = torch.zeros_like(unlisted).scatter_(1, idx.long(), q)
+    want = torch.where(listed, p - dense, unlisted) * (g.double() / T)[:, None]
+    w = (q_r.log() - log_s).abs()
+    log_ratio = q_r.log() - log_rest
+    steps = L + 16 + 4 * d.clamp(min=-1e4).abs() + 4 * w + torch.where(log_ratio.abs() < 300, 8 * log_ratio.abs(), 0.0)
+    small = (within * log_rest.exp() + q_r * within) * steps * U
+    tol = torch.where(listed, (p + dense) * (4 * 40 + L + 16) * U, small) * (g.double() / T)[:, None]
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    for name, x in (("alone", got), ("added", added)):
+        off = (x.double() - want).abs()
+        bound = tol + half * (want.abs() + tol) + 2.0 ** -126
+        assert bool(torch.isfinite(x).all()), name
+        assert bool((off <= bound).all()), (name, float((off / bound).max()), int((off / bound).amax(1).argmax()) % 8)
