@@ -508,7 +508,7 @@ class Camera:
         pre = torch.empty((n, 2, (d_ff + 7) // 8 * 8), dtype=torch.float32, device=self.device) if want_pre else None
         self._check(self.lib.camera_gated_ffn(
             self._ctx, _stream_handle(self.device), _ptr(X), _dtype_code(X), n, X.shape[1], _row_stride(X), _ptr(W_gate), _ptr(W_up),
-            d_ff, _ptr(H), H.stride(0) if n > 1 else max(H.stride(0), d_ff), _ptr(pre)))
+            d_ff, _ptr(H), H.stride(0) if n > 1 else whole, _ptr(pre)))  # a single row has no stride
         return (H, pre) if want_pre else H
 
     def gated_ffn_backward(self, X, W_gate, W_up, dH, pre=None, want=(True, True, True)):

@@ -53,3 +53,20 @@ def test_a_given_block_is_not_written_beyond_its_buffer(host, d_ff, dtype):
         room = H.untyped_storage().nbytes() // H.element_size() - H.storage_offset()
         assert refused or (n - 1) * a["ldh"] + whole <= room, (tuple(H.stride()), a["ldh"])
         assert refused == (H.stride(0) < d_ff or H.stride(0) % v != 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_single_row_has_no_stride(host, dtype):
+    """Whatever torch leaves as the stride of one row: its address counts, and that a whole number of vectors fits behind it."""
+    v = 128 // torch.finfo(dtype).bits
+    for d_ff in (20, 13, 24):
+        whole = -(-d_ff // v) * v
+        buf = torch.zeros(whole, dtype=dtype)
+        for stride in (0, 1, d_ff, whole, 67):
+            host.gated_ffn(*block(1, d_ff, dtype), H=buf.as_strided((1, d_ff), (stride, 1)))
+            assert host.lib.args["ldh"] >= d_ff and host.lib.args["ldh"] % v == 0, stride
+        if whole > d_ff:
+            with pytest.raises(binding.CameraError, match="last row"):
+                host.gated_ffn(*block(1, d_ff, dtype), H=torch.zeros(d_ff, dtype=dtype).view(1, d_ff))
+    host.gated_ffn(*block(0, 13, dtype), H=torch.zeros((0, 13), dtype=dtype))
+    assert host.lib.args["ldh"] % v == 0
