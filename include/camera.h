@@ -394,7 +394,7 @@ int camera_output_error(camera_ctx* ctx, void* stream, const float* Y, const flo
  *   logits   [n x vocab], row stride ld >= vocab elements, `dtype`; rows may start at any element.  A logit of -Inf rules a
  *            token out.  A row that rules every token out: entropy 0, stats -Inf and 0, logprob -Inf.  NaN or +Inf in a row:
  *            that row's results are unspecified (its indices are tokens or -1).
- *   temperature  > 0, finite
+ *   temperature  > 0, finite, log2(e) / temperature too (from 4.3e-39 on)
  *   targets  int32 [n]; a value outside [0, vocab) stands for a position without target: logprob 0.  NULL with logprob NULL.
  *   top_k    in [0, min(vocab, CAMERA_MAX_ALTERNATIVES)]; 0: top_idx and top_logprob are not written (may be NULL)
  *   logprob, entropy float32 [n], stats float32 [n x 2], top_idx int32 [n x top_k], top_logprob float32 [n x top_k] out; each of

@@ -1088,8 +1088,9 @@ int check_logits(camera_ctx* ctx, const void* logits, int dtype, int64_t n, int6
   if (vocab < 1 || vocab >= (int64_t(1) << 31) - 1024) return fail(ctx, CAMERA_ESHAPE, "vocab: must be in [1, 2^31 - 1024)");
   if (n >= int64_t(1) << 31) return fail(ctx, CAMERA_ESHAPE, "n: must be below 2^31");
   if (ld < vocab) return fail(ctx, CAMERA_ESHAPE, "ld: must be >= vocab");
-  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature))
-    return fail(ctx, CAMERA_EINVAL, "temperature: must be positive and finite, its reciprocal too");
+  // the kernels take exponents in powers of two: log2(e) / temperature times a difference of logits, 0 among them
+  if (!(temperature > 0.0f) || !std::isfinite(temperature) || !std::isfinite(1.4427f / temperature))
+    return fail(ctx, CAMERA_EINVAL, "temperature: must be positive and finite, log2(e) / temperature too");
   if (n > 0 && logits == nullptr) return fail(ctx, CAMERA_EINVAL, "logits: NULL");
   if (!aligned_to(logits, dtype == CAMERA_BF16 ? 2 : 4)) return fail(ctx, CAMERA_ESHAPE, "logits: not aligned to an element");
   return CAMERA_OK;
