@@ -25,7 +25,7 @@
  *     the workspace: a graph captured before it must not be replayed after it,
  *     so make the largest call of every kind before the first capture.
  *   - NaN / Inf in the inputs: results unspecified (not checked).  (The calls on
- *     logits say what -Inf means there.)
+ *     logits say what they mean there.)
  *   - Device data pointers must be 16-byte aligned; for CAMERA_BF16 d_model and
  *     ldx must be multiples of 8, for CAMERA_F32 multiples of 4.  (The calls on
  *     logits take rows that start at any element.)
@@ -393,7 +393,7 @@ int camera_output_error(camera_ctx* ctx, void* stream, const float* Y, const flo
  *
  *   logits   [n x vocab], row stride ld >= vocab elements, `dtype`; rows may start at any element.  A logit of -Inf rules a
  *            token out.  A row that rules every token out: entropy 0, stats -Inf and 0, logprob -Inf.  NaN or +Inf in a row:
- *            that row's results are unspecified (its indices are tokens or -1).
+ *            entropy, the second of stats, the target's logprob and the alternatives' log p are NaN (their indices tokens, or -1).
  *   temperature  > 0, finite, log2(e) / temperature too (from 4.3e-39 on)
  *   targets  int32 [n]; a value outside [0, vocab) stands for a position without target: logprob 0.  NULL with logprob NULL.
  *   top_k    in [0, min(vocab, CAMERA_MAX_ALTERNATIVES)]; 0: top_idx and top_logprob are not written (may be NULL)
@@ -411,7 +411,8 @@ int camera_output_error(camera_ctx* ctx, void* stream, const float* Y, const flo
  *   dlogits          [n x vocab], row stride ldd >= vocab, `dtype`, out (elements behind a row's end are left alone).  Without
  *            CAMERA_ACCUMULATE it may be `logits` itself (ldd == ld then); any other overlap is not allowed.
  * Each value is computed in float32 and rounded once to `dtype` (with CAMERA_ACCUMULATE after the addition).  Rows without gradient
- * (both factors 0) are set to 0 without reading their logits; so are rows that rule every token out.
+ * (both factors 0) are set to 0 without reading their logits; so are rows that rule every token out.  A row with NaN or +Inf among
+ * its logits has a gradient of NaN, all of it.
  */
 int camera_token_logprobs(camera_ctx* ctx, void* stream,
                           const void* logits, int dtype, int64_t n, int64_t vocab, int64_t ld, float temperature,
@@ -438,6 +439,7 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
  *   teacher_logprob  float32 [n x k]; an entry of -Inf is ignored.  1 <= k <= CAMERA_MAX_ALTERNATIVES.
  *   loss   float32 [n] out.  A row without entries has loss 0 (with CAMERA_DISTILL_TAIL: all of its probability is in the one
  *            class, loss 0).  +Inf where a listed token with q_j > 0 has logit -Inf (its gradient is what the formula gives: finite).
+ *            NaN where there is NaN or +Inf among the row's logits (and an entry counts, or the class), and its gradient too.
  *   stats  float32 [n x CAMERA_DISTILL_STATS] out, for the gradient: max of the logits, log sum exp((z - max) / temperature),
  *            log sum exp(teacher_logprob / temperature) (0 with CAMERA_DISTILL_TAIL), the sum of q, and log(q_r / p_r) (-Inf
  *            without that class): an unlisted token's part of the gradient is p (sum of q - q_r / p_r)

@@ -5,7 +5,8 @@
 //   log p_v = (z_v - m) / T - log S,      H = -sum p log p = log S - (1 / S) sum exp(d_v) d_v,  d_v = (z_v - m) / T
 // One pass over a row keeps, per thread, the largest logit so far, the sum of exponentials relative to it and the sum weighted
 // by the exponents, all in float32, and rescales the sums when the largest logit grows.  d_v is taken as a difference first, so
-// that logits of any size (the type's lowest value as a mask among them) stay exact; a logit of -inf adds nothing.
+// that logits of any size (the type's lowest value as a mask among them) stay exact; a logit of -inf adds nothing.  A NaN, or the
+// difference of two infinities, stays in the sums and makes the row's results NaN; only the maxima pass it over.
 //
 // All of it is bound by reading the logits once (and writing the gradient once).  bf16, 4096 rows of 151936: log probabilities, entropy and
 // 64 alternatives 228 us (5.5 TB/s), distillation with 64 listed tokens and the rest as a class 217 us (5.8), gradients of 2048 rows
@@ -27,6 +28,7 @@ constexpr int kShortVocab = 16384, kShortTop = 64;  // longest row and most alte
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.693147180559945309417f;
 constexpr float kFloor = -1.0e4f;  // exponents are clamped here: exp2 of it is 0, and 0 times it is 0
+__device__ __forceinline__ float floored(float d) { return __builtin_elementwise_maximum(d, kFloor); }  // NaN stays NaN, one instruction
 static_assert(kLong >= CAMERA_MAX_ALTERNATIVES && kShort >= kShortTop, "the k-th largest of the threads' maxima exists");
 
 // 16 bytes of a row.  Rows start where the caller's do, at any element: the loads and stores carry the element's alignment only.
@@ -108,6 +110,9 @@ struct Running {
 };
 // What an empty row or thread is taken relative to.
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
+// Nothing but logits of -inf: any other adds at least the largest one's 1, or NaN.
+__device__ __forceinline__ bool nothing(const Running& r) { return r.s == 0.0f; }
+__device__ __forceinline__ float log_sum_of(const Running& r) { return nothing(r) ? 0.0f : logf(r.s); }
 // The sums relative to the larger maximum `m`.
 __device__ __forceinline__ void rescale(Running& r, float m, float scale) {
   const float d = fmaxf((r.m - reference(m)) * scale, kFloor), c = __builtin_amdgcn_exp2f(d);
@@ -126,7 +131,9 @@ __device__ __forceinline__ float add_values(Running& r, const float* z, float sc
   const float ref = reference(m);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float d = fmaxf((z[i] - ref) * scale, kFloor), e = __builtin_amdgcn_exp2f(d);
+    float d = (z[i] - ref) * scale;
+    if constexpr (ENTROPY) d = floored(d);  // 0 times -inf would not be 0
+    const float e = __builtin_amdgcn_exp2f(d);
     r.s += e;
     if constexpr (ENTROPY) r.t = fmaf(e, d, r.t);
   }
@@ -496,8 +503,8 @@ __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, 
 // ---- log probabilities, entropy, alternatives ----------------------------------------------------------------------
 template <class T>
 __device__ __forceinline__ void finish_logprobs(const Running& r, const LogprobArgs& a, int64_t row) {
-  const bool none = r.m == -INFINITY;
-  const float log_sum = none ? 0.0f : logf(r.s);
+  const bool none = nothing(r);
+  const float log_sum = log_sum_of(r);
   if (threadIdx.x == 0) {
     if (a.stats) {
       a.stats[2 * row] = r.m;
@@ -545,7 +552,7 @@ __global__ __launch_bounds__(TH, 4) void logprobs_kernel(LogprobArgs a) {
   if constexpr (WHOLE) finish_logprobs<T>(r, a, row);
   else if (threadIdx.x == 0) a.part_stats[block] = make_float4(r.m, r.s, r.t, 0.0f);
   if constexpr (TOP) {
-    const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
+    const float log_sum = log_sum_of(r);
     select_top<TH>(LogitKeys<T, TH>{p}, order_bits(mine.m), a.top_k, *select, [&](int place, uint64_t key) {
       if constexpr (WHOLE) write_alternative(a, r, log_sum, row, place, key);
       else a.part_keys[block * a.top_k + place] = key;
@@ -582,7 +589,7 @@ __global__ __launch_bounds__(kLong) void logprobs_join_kernel(LogprobArgs a) {
   finish_logprobs<T>(r, a, row);
   if constexpr (TOP) {
     __shared__ SelectSmem<TH> sm;
-    const float log_sum = r.m == -INFINITY ? 0.0f : logf(r.s);
+    const float log_sum = log_sum_of(r);
     const ListKeys<TH> keys{a.part_keys + row * a.parts * a.top_k, a.parts * a.top_k};
     uint32_t largest = 0;
     for (int pos = 0; pos < keys.positions(); ++pos) keys.at(threadIdx.x, 0, pos, [&](uint32_t bits, int) { largest = max(largest, bits); });
@@ -676,7 +683,7 @@ __global__ __launch_bounds__(TH) void logprobs_grad_kernel(LogitGradArgs a, cons
   const float m = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
   const float one = grad_logprob && target >= 0 && target < a.vocab ? grad_logprob[row] * a.inv_temperature : 0.0f;
   const float two = grad_entropy ? grad_entropy[row] * a.inv_temperature : 0.0f;
-  if ((one == 0.0f && two == 0.0f) || m == -INFINITY) {  // the gradient is 0 whatever the logits are
+  if ((one == 0.0f && two == 0.0f) || (m == -INFINITY && log_sum == 0.0f)) {  // no gradient, or nothing but -inf
     if (!p.accumulate) p.zero();
     return;
   }
@@ -687,7 +694,7 @@ __global__ __launch_bounds__(TH) void logprobs_grad_kernel(LogitGradArgs a, cons
     constexpr int N = decltype(count)::value;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float lp = fmaxf((x[i] - m) * inv_t - log_sum, kFloor);
+      const float lp = floored((x[i] - m) * inv_t - log_sum);
       x[i] = __builtin_amdgcn_exp2f(lp * kLog2e) * -fmaf(two, lp + h, one);
     }
     if (one != 0.0f && at >= v && at < v + N) {
@@ -783,9 +790,9 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
     double listed = 0.0;
 #pragma unroll
     for (int e = 0; e < kEntries; ++e)
-      if (z[e] > -INFINITY) listed += exp(((double)z[e] - ref) * inv_t);
+      if (z[e] != -INFINITY) listed += exp(((double)z[e] - ref) * inv_t);
     sum = wave_all(listed, Add{});
-    if (rest.m > -INFINITY) sum += (double)rest.s * exp(((double)rest.m - ref) * inv_t);
+    if (!nothing(rest)) sum += (double)rest.s * exp(((double)rest.m - ref) * inv_t);
   } else {
     const double ref = reference(wave_all(value_max, Max{}));
     double total = 0.0;
@@ -795,19 +802,19 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
     total = wave_all(total, Add{});
     if (total > 0.0) norm = ref * inv_t + log(total);
   }
-  if (m > -INFINITY) log_sum = log(sum);
+  if (sum != 0.0) log_sum = log(sum);
   double loss = 0.0, mass = 0.0, log_ratio = -INFINITY;
 #pragma unroll
   for (int e = 0; e < kEntries; ++e)
     if (ok[e]) {
       const double log_q = a.tail ? (double)value[e] : (double)value[e] * inv_t - norm, q = exp(log_q);
-      const double log_p = z[e] > -INFINITY ? ((double)z[e] - (double)m) * inv_t - log_sum : -INFINITY;
+      const double log_p = ((double)z[e] - (double)reference(m)) * inv_t - log_sum;
       mass += q;
       if (q > 0.0) loss += q * (log_q - log_p);
     }
   loss = wave_all(loss, Add{});
   mass = wave_all(mass, Add{});
-  if (a.tail && rest.m > -INFINITY) {
+  if (a.tail && !nothing(rest)) {
     const double left = fmax(0.0, 1.0 - mass);
     const double log_rest = ((double)rest.m - (double)m) * inv_t + log((double)rest.s) - log_sum;
     mass += left;
@@ -887,7 +894,7 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
   const float* st = a.stats + row * CAMERA_DISTILL_STATS;
   const float m = st[0], log_sum = st[1], norm = st[2], mass = st[3], log_ratio = st[4];
   const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
-  if (g == 0.0f || m == -INFINITY) {  // the gradient is 0 whatever the logits are
+  if (g == 0.0f || (m == -INFINITY && log_sum == 0.0f)) {  // no gradient, or nothing but -inf
     if (!p.accumulate) p.zero();
     return;
   }
@@ -904,7 +911,7 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
     listed[e] = 0.0f;
     if (at[e] >= 0) {
       const float value = list.value[j];
-      const float lp = fmaxf((Pack<T>::one(p.z[at[e]]) - m) * inv_t - log_sum, kFloor);
+      const float lp = floored((Pack<T>::one(p.z[at[e]]) - m) * inv_t - log_sum);
       const float lq = tail ? value : value * inv_t - norm;
       listed[e] = g * (mass * expf(lp) - expf(lq));
       if (p.accumulate) listed[e] += Pack<T>::one(p.out[at[e]]);
