@@ -442,7 +442,9 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
  *            NaN where there is NaN or +Inf among the row's logits (and an entry counts, or the class), and its gradient too.
  *   stats  float32 [n x CAMERA_DISTILL_STATS] out, for the gradient: max of the logits, log sum exp((z - max) / temperature),
  *            log sum exp(teacher_logprob / temperature) (0 with CAMERA_DISTILL_TAIL), the sum of q, and log(q_r / p_r) (-Inf
- *            without that class): an unlisted token's part of the gradient is p (sum of q - q_r / p_r)
+ *            without that class): an unlisted token's part of the gradient is p (sum of q - q_r / p_r).  Where the last is above 256
+ *            (the sum of q is 1 then), the third is the largest unlisted logit m_r and the fourth log q_r - log sum exp((z - m_r) / T) over
+ *            the unlisted: the gradient by the ratio would be off by the ratio's logarithm
  * The vocabulary's sums are taken in float32, those over the listed tokens in float64.  The workspace of a call serves every
  * other, unless with CAMERA_DISTILL_TAIL vocab is above 2^18, where it grows with n.  n == 0 does nothing.
  *

@@ -711,6 +711,11 @@ __global__ __launch_bounds__(TH) void logprobs_grad_kernel(LogitGradArgs a, cons
 //   loss = sum_j q_j (log q_j - log p_j)  [+ q_r (log q_r - log p_r)],  q_r = 1 - sum q_j,  p_r = sum of p_v over the unlisted v
 // p_r is summed over the unlisted tokens themselves (1 - sum p_j would cancel): a bit per token of the part marks the listed ones.
 // The few values of the listed tokens are handled in float64.
+// The gradient takes the class by log(q_r / p_r), as a float32 off by u of itself and the exponents with it.  Beyond kFarClass (all
+// unlisted tokens masked by -1e4 or the type's lowest value: off by anything up to infinity) it takes the class by itself instead:
+// p_v q_r / p_r = q_r exp((z_v - m_r) / T) / S_r with the class's own maximum and sum, beside which p_v is nothing.  stats have no more
+// room, but for the two that then are known: norm (0 with tail) and the sum of q (1) hold m_r and log(q_r / S_r).
+constexpr float kFarClass = 256.0f;
 
 // A row's teacher list in LDS, id -1 where an entry does not count: it names no token, has no probability, or an entry before it
 // names the same token.
@@ -814,8 +819,9 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
     }
   loss = wave_all(loss, Add{});
   mass = wave_all(mass, Add{});
+  double left = 0.0;
   if (a.tail && !nothing(rest)) {
-    const double left = fmax(0.0, 1.0 - mass);
+    left = fmax(0.0, 1.0 - mass);
     const double log_rest = ((double)rest.m - (double)m) * inv_t + log((double)rest.s) - log_sum;
     mass += left;
     if (left > 0.0) {
@@ -828,8 +834,9 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
     float* st = a.stats + row * CAMERA_DISTILL_STATS;
     st[0] = m;
     st[1] = (float)log_sum;
-    st[2] = (float)norm;
-    st[3] = (float)mass;
+    const bool far = log_ratio > kFarClass;
+    st[2] = far ? rest.m : (float)norm;
+    st[3] = far ? (float)log(left / (double)rest.s) : (float)mass;
     st[4] = (float)log_ratio;
   }
 }
@@ -892,7 +899,9 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
   if (row >= a.n) return;
   GradPart<T, TH> p = grad_part<T, TH>(a, row, (int)(block - row * a.parts));
   const float* st = a.stats + row * CAMERA_DISTILL_STATS;
-  const float m = st[0], log_sum = st[1], norm = st[2], mass = st[3], log_ratio = st[4];
+  const float m = st[0], log_sum = st[1], norm = st[2], log_ratio = st[4];
+  const bool far = log_ratio > kFarClass;
+  const float mass = far ? 1.0f : st[3];
   const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
   if (g == 0.0f || (m == -INFINITY && log_sum == 0.0f)) {  // no gradient, or nothing but -inf
     if (!p.accumulate) p.zero();
@@ -919,12 +928,14 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
   }
   __syncthreads();  // the reads above are done before the part is written
   // p_v (mass - q_r / p_r) as one exponential: the ratio may be as large as p_r is small, and mass is then nothing beside it
-  const float scale2 = inv_t * kLog2e, factor = mass - expf(log_ratio), c = factor < 0.0f ? -g : g;
-  const float log2_factor = factor == 0.0f ? kFloor : (log_ratio > 80.0f ? log_ratio : logf(fabsf(factor))) * kLog2e - log_sum * kLog2e;
+  const float scale2 = inv_t * kLog2e, factor = mass - expf(log_ratio), c = factor < 0.0f ? -g : g, from = far ? st[2] : m;
+  const float log2_factor = far              ? st[3] * kLog2e
+                            : factor == 0.0f ? kFloor
+                                             : (log_ratio > 80.0f ? log_ratio : logf(fabsf(factor))) * kLog2e - log_sum * kLog2e;
   p.each([&](float* x, int, auto count) {
     constexpr int N = decltype(count)::value;
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = c * __builtin_amdgcn_exp2f(fmaf(x[i] - m, scale2, log2_factor));
+    for (int i = 0; i < N; ++i) x[i] = c * __builtin_amdgcn_exp2f(fmaf(x[i] - from, scale2, log2_factor));
   });
   __syncthreads();  // and written before the listed tokens are
 #pragma unroll

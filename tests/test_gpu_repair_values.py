@@ -87,3 +87,68 @@ def test_distillation_shows_nan(cam, n, vocab, tail, dtype):
     for key in good:
         assert torch.equal(out[key][~spoiled], good[key][~spoiled]), key
     assert torch.equal(got[~spoiled], want[~spoiled])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1.0, 0.5, 2.0])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_unlisted_class_next_to_impossible(cam, n, vocab, T, dtype):
+    """The student keeps the listed tokens and gives all others a mask's value (rows: -50, -200, -1e3, -1e4, -1e9, the type's lowest,
+    the last two with a few tokens less ruled out), the teacher has a quarter of its probability there.  The unlisted tokens' gradient is
+    p - q_r softmax(unlisted): about -1 / (4 unlisted) each, whatever the mask.
+
+    Tolerance, relative to the two terms: L additions in each sum, 4 u per unit of the exponents that are taken, d from the class's largest
+    logit, w = log q_r - log sum exp d; where the class is within e^-256 its ratio to q_r goes through float32 as a logarithm, 4 u each unit."""
+    k = 8
+    z = rows_of(n, vocab, dtype, 4)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    idx = torch.stack([torch.randperm(vocab, generator=gen, device="cuda")[:k] for _ in range(8)]).repeat(-(-n // 8), 1)[:n].int()
+    lowest = torch.finfo(TYPES[dtype]).min
+    masks = [-50.0, -200.0, -1e3, -1e4, -1e9, lowest, -1e9, lowest]
+    listed = torch.zeros((n, vocab), dtype=torch.bool, device="cuda").scatter_(1, idx.long(), True)
+    some = torch.rand(vocab, generator=gen, device="cuda") < 0.3
+    noise = 2 * torch.rand((n, vocab), generator=gen, device="cuda")
+    for i, value in enumerate(masks):
+        fill = torch.full((vocab,), value, device="cuda")
+        if value > -1e5:
+            fill = fill - noise[i]                         # not all alike where the type can tell
+        elif i >= 6:
+            fill[some] = value / 2
+        z[i::8] = torch.where(listed[i::8], z[i::8], fill.to(TYPES[dtype]))
+    share = torch.rand((n, k), generator=gen, device="cuda") + 0.1
+    val = (0.75 * share / share.sum(1, keepdim=True)).log()
+    g = torch.linspace(0.5, 2.0, n, device="cuda")
+    out = cam.distill_topk(z, idx, val, temperature=T, tail=True)
+    got = cam.distill_topk_backward(z, idx, val, out["stats"], g, temperature=T, tail=True)
+    added = cam.distill_topk_backward(z, idx, val, out["stats"], g, temperature=T, tail=True, dlogits=torch.zeros_like(z), accumulate=True)
+    torch.cuda.synchronize()
+
+    d = z.double().masked_fill(listed, -math.inf)
+    m_r = d.amax(1, keepdim=True)
+    d = (d - m_r) / T
+    log_s = torch.logsumexp(d, 1, keepdim=True)
+    here = z.double().gather(1, idx.long()) / T
+    log_sum = torch.logaddexp(torch.logsumexp(here, 1, keepdim=True), m_r / T + log_s)
+    q = val.double().exp()
+    q_r = 1 - q.sum(1, keepdim=True)
+    log_rest = m_r / T + log_s - log_sum
+    loss = (q * (val.double() - (here - log_sum))).sum(1) + (q_r * (q_r.log() - log_rest))[:, 0]
+    L = vocab / 128 + 40
+    fits = loss < 3e38
+    assert bool(((out["loss"].double() - loss).abs()[fits] <= ((L + 32) * U + 4 * U * loss.abs())[fits]).all())
+    within = (d - log_s).exp()                              # of the class; 0 at the listed tokens
+    unlisted = within * log_rest.exp() - q_r * within
+    p = torch.zeros_like(unlisted).scatter_(1, idx.long(), (here - log_sum).exp())
+    dense = torch.zeros_like(unlisted).scatter_(1, idx.long(), q)
+    want = torch.where(listed, p - dense, unlisted) * (g.double() / T)[:, None]
+    w = (q_r.log() - log_s).abs()
+    log_ratio = q_r.log() - log_rest
+    steps = L + 16 + 4 * d.clamp(min=-1e4).abs() + 4 * w + torch.where(log_ratio.abs() < 300, 8 * log_ratio.abs(), 0.0)
+    small = (within * log_rest.exp() + q_r * within) * steps * U
+    tol = torch.where(listed, (p + dense) * (4 * 40 + L + 16) * U, small) * (g.double() / T)[:, None]
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    for name, x in (("alone", got), ("added", added)):
+        off = (x.double() - want).abs()
+        bound = tol + half * (want.abs() + tol) + 2.0 ** -126
+        assert bool(torch.isfinite(x).all()), name
+        assert bool((off <= bound).all()), (name, float((off / bound).max()), int((off / bound).amax(1).argmax()) % 8)
