@@ -433,7 +433,8 @@ int camera_token_logprobs_backward(camera_ctx* ctx, void* stream,
  *            temperature 1 (those taken at this temperature, as CAMERA_DISTILL_TAIL wants them, times the temperature do as well)
  *   flags CAMERA_DISTILL_TAIL  q_j = exp(teacher_logprob_j), which were taken at this temperature, and all tokens that are not
  *            listed are one more class: + q_r (log q_r - log p_r), q_r = max(0, 1 - sum q_j), p_r = the sum of their p.  Where no
- *            token is left for it the class drops out.
+ *            token is left for it the class drops out, and so it does with q_r < 2^-20 and p_r < q_r e^-256: the tokens that a mask of
+ *            any number leaves are all listed, and q_r is what rounding their log probabilities leaves of 1.
  *   logits, temperature   as in camera_token_logprobs
  *   teacher_idx      int32 [n x k]; an entry outside [0, vocab) is ignored, and so is one that repeats an earlier entry of its row
  *   teacher_logprob  float32 [n x k]; an entry of -Inf is ignored.  1 <= k <= CAMERA_MAX_ALTERNATIVES.

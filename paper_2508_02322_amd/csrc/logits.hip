@@ -716,6 +716,9 @@ __global__ __launch_bounds__(TH) void logprobs_grad_kernel(LogitGradArgs a, cons
 // p_v q_r / p_r = q_r exp((z_v - m_r) / T) / S_r with the class's own maximum and sum, beside which p_v is nothing.  stats have no more
 // room, but for the two that then are known: norm (0 with tail) and the sum of q (1) hold m_r and log(q_r / S_r).
 constexpr float kFarClass = 256.0f;
+// Such a class with less than this of the teacher is none: it is what the roundings of the listed log probabilities leave of 1 (each
+// is off by about 4 u of it, together up to 16 u), and times the logarithm of a mask it would be the loss (1e31 for the type's lowest).
+constexpr double kNoClass = 0x1p-20;
 
 // A row's teacher list in LDS, id -1 where an entry does not count: it names no token, has no probability, or an entry before it
 // names the same token.
@@ -823,11 +826,13 @@ __device__ __forceinline__ void finish_distill(const Running& rest, const Distil
   if (a.tail && !nothing(rest)) {
     left = fmax(0.0, 1.0 - mass);
     const double log_rest = ((double)rest.m - (double)m) * inv_t + log((double)rest.s) - log_sum;
-    mass += left;
-    if (left > 0.0) {
-      log_ratio = log(left) - log_rest;
-      loss += left * log_ratio;
+    log_ratio = log(left) - log_rest;  // -inf where nothing is left
+    if (log_ratio > (double)kFarClass && left < kNoClass) {
+      left = 0.0;
+      log_ratio = -INFINITY;
     }
+    mass += left;
+    if (left > 0.0) loss += left * log_ratio;
   }
   if (lane == 0) {
     a.loss[row] = (float)loss;

@@ -152,3 +152,41 @@ def test_unlisted_class_next_to_impossible(cam, n, vocab, T, dtype):
         bound = tol + half * (want.abs() + tol) + 2.0 ** -126
         assert bool(torch.isfinite(x).all()), name
         assert bool((off <= bound).all()), (name, float((off / bound).max()), int((off / bound).amax(1).argmax()) % 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [-1e4, -1e9, "lowest", -math.inf])
+@pytest.mark.parametrize("left,k", [(1, 4), (5, 20), (30, 64), (60, 64)])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_both_models_masked_alike(cam, n, vocab, left, k, value, dtype):
+    """A mask leaves the same few tokens to both models, fewer than the list is long: nothing is left for the unlisted class but the
+    rounding of the teacher's log probabilities, and the divergence is that of the few tokens, whatever number the mask is.
+
+    Tolerance: the teacher's and the student's log probabilities are off by (4 |lp| + L + 8) u each, L = left additions of numbers
+    that are not 0 and 4 levels of the join."""
+    mask = torch.finfo(TYPES[dtype]).min if value == "lowest" else value
+    original, z = rows_of(n, vocab, dtype, 7), rows_of(n, vocab, dtype, 8)
+    out = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    out[torch.randperm(vocab, generator=torch.Generator(device="cuda").manual_seed(9), device="cuda")[:left]] = False
+    original[:, out] = mask
+    z[:, out] = mask
+    g = torch.ones(n, device="cuda")
+    for T in (1.0, 2.0):
+        top = cam.token_logprobs(original, top_k=k, temperature=T)
+        teacher = top["top_idx"], top["top_logprob"]
+        kd = cam.distill_topk(z, *teacher, temperature=T, tail=True)
+        got = cam.distill_topk_backward(z, *teacher, kd["stats"], g, temperature=T, tail=True)
+        torch.cuda.synchronize()
+        lq, lp = (torch.log_softmax(x[:, ~out].double() / T, 1) for x in (original, z))
+        off = lambda t: (4 * t.abs() + left + 12) * U  # noqa: E731
+        kl = (lq.exp() * (lq - lp)).sum(1)
+        tol = (lq.exp() * (off(lq) * (1 + (lq - lp).abs()) + off(lp))).sum(1) + U * kl.abs() + 2.0 ** -20
+        assert bool(((kd["loss"].double() - kl).abs() <= tol).all()), (T, float((kd["loss"].double() - kl).abs().max()))
+        want = torch.zeros((n, vocab), dtype=torch.float64, device="cuda")
+        want[:, ~out] = (lp.exp() - lq.exp()) / T
+        size = torch.zeros_like(want)
+        size[:, ~out] = (lp.exp() * off(lp) + lq.exp() * off(lq) + 8 * U) / T
+        half = torch.finfo(TYPES[dtype]).eps / 2
+        # q_r is at most 2^-20, over the unlisted tokens, where it is not told from rounding
+        bound = size + half * (want.abs() + size) + 2.0 ** -20 / T
+        assert bool(((got.double() - want).abs() <= bound).all()), float((got.double() - want).abs().max())
