@@ -892,6 +892,26 @@ __global__ __launch_bounds__(kLong) void distill_join_kernel(DistillArgs a) {
   if (threadIdx.x < kWave) finish_distill<T>(r, a, row, teacher);
 }
 
+// The largest of the values that count, and 1 over the sum of exp((value - that) / T), for a wave of its own accord (a part of a row
+// has few waves with listed tokens, most none).  From the values and not from their norm in stats: a float32 of values far from 0 is
+// off by more than their differences.
+__device__ __forceinline__ void list_softmax(const TeacherSmem& list, int k, float scale, float& value_max, float& share) {
+  constexpr int kEntries = CAMERA_MAX_ALTERNATIVES / kWave;
+  const int lane = threadIdx.x % kWave;
+  float value[kEntries], most = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < kEntries; ++e) {
+    const int j = e * kWave + lane;
+    value[e] = j < k && list.id[j] >= 0 ? list.value[j] : -INFINITY;
+    most = fmaxf(most, value[e]);
+  }
+  most = wave_all(most, Max{});
+#pragma unroll
+  for (int e = 0; e < kEntries; ++e) sum += __builtin_amdgcn_exp2f((value[e] - most) * scale);  // 0 where there is none
+  value_max = most;
+  share = 1.0f / wave_all(sum, Add{});
+}
+
 // d loss / dz_v = (mass p_v - q_v) / T for a listed v, p_v (mass - q_r / p_r) / T for an unlisted one (mass alone without tail):
 // the second for every token of the part, then the first over the listed ones.  A listed token's logit and old gradient
 // are read before anything is written (dlogits may be logits), and its value is written after the workgroup's stores are done.
@@ -904,7 +924,7 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
   if (row >= a.n) return;
   GradPart<T, TH> p = grad_part<T, TH>(a, row, (int)(block - row * a.parts));
   const float* st = a.stats + row * CAMERA_DISTILL_STATS;
-  const float m = st[0], log_sum = st[1], norm = st[2], log_ratio = st[4];
+  const float m = st[0], log_sum = st[1], log_ratio = st[4];
   const bool far = log_ratio > kFarClass;
   const float mass = far ? 1.0f : st[3];
   const float inv_t = a.inv_temperature, g = grad_loss[row] * inv_t;
@@ -917,23 +937,31 @@ __global__ __launch_bounds__(TH) void distill_grad_kernel(LogitGradArgs a, Disti
   constexpr int kEach = (CAMERA_MAX_ALTERNATIVES + TH - 1) / TH;  // entries of a thread
   int64_t at[kEach];
   float listed[kEach];
+  bool any = false;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
     const int j = threadIdx.x + e * TH;
     at[e] = j < teacher.k && list.id[j] >= 0 ? list.id[j] - p.first : -1;
     if (at[e] >= p.len) at[e] = -1;
+    any = any || at[e] >= 0;
+  }
+  const float scale2 = inv_t * kLog2e;
+  float value_max = 0.0f, share = 1.0f;  // q_j = share exp((value_j - value_max) / T), or with tail exp(value_j)
+  if (!tail && __any(any)) list_softmax(list, teacher.k, scale2, value_max, share);
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
     listed[e] = 0.0f;
     if (at[e] >= 0) {
-      const float value = list.value[j];
+      const float value = list.value[threadIdx.x + e * TH];
       const float lp = floored((Pack<T>::one(p.z[at[e]]) - m) * inv_t - log_sum);
-      const float lq = tail ? value : value * inv_t - norm;
-      listed[e] = g * (mass * expf(lp) - expf(lq));
+      const float q = share * (tail ? expf(value) : __builtin_amdgcn_exp2f((value - value_max) * scale2));
+      listed[e] = g * (mass * expf(lp) - q);
       if (p.accumulate) listed[e] += Pack<T>::one(p.out[at[e]]);
     }
   }
   __syncthreads();  // the reads above are done before the part is written
   // p_v (mass - q_r / p_r) as one exponential: the ratio may be as large as p_r is small, and mass is then nothing beside it
-  const float scale2 = inv_t * kLog2e, factor = mass - expf(log_ratio), c = factor < 0.0f ? -g : g, from = far ? st[2] : m;
+  const float factor = mass - expf(log_ratio), c = factor < 0.0f ? -g : g, from = far ? st[2] : m;
   const float log2_factor = far              ? st[3] * kLog2e
                             : factor == 0.0f ? kFloor
                                              : (log_ratio > 80.0f ? log_ratio : logf(fabsf(factor))) * kLog2e - log_sum * kLog2e;

@@ -190,3 +190,64 @@ def test_both_models_masked_alike(cam, n, vocab, left, k, value, dtype):
         # q_r is at most 2^-20, over the unlisted tokens, where it is not told from rounding
         bound = size + half * (want.abs() + size) + 2.0 ** -20 / T
         assert bool(((got.double() - want).abs() <= bound).all()), float((got.double() - want).abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3e38, 1e30, 1e-30, 5e-39])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_temperatures_at_the_ends(cam, n, vocab, T, dtype):
+    """All tokens that are left alike, or the largest alone; ruled out ones stay so.  log of up to 17001 terms of 1: (L + 8) u off,
+    16 u for a value below 16, and the same for the distance from the largest's difference, 0."""
+    z = rows_of(n, vocab, dtype, 6)
+    z[:, 7::3] = -math.inf
+    z[:, 100] = 40.0
+    left = (z[0] != -math.inf).sum().double()
+    targets = torch.full((n,), 100, dtype=torch.int32, device="cuda")
+    idx = torch.tensor([[100, 0, 1]], dtype=torch.int32, device="cuda").repeat(n, 1)
+    val = torch.full((n, 3), -math.log(4.0), device="cuda")
+    out = cam.token_logprobs(z, targets, top_k=3, temperature=T)
+    g = torch.ones(n, device="cuda") * min(T, 1.0)                     # the gradient is 1 / T long
+    grad = cam.token_logprobs_backward(z, targets, out["stats"], g, temperature=T)
+    kd = [cam.distill_topk(z, idx, val, temperature=T, tail=tail) for tail in (False, True)]
+    kd_grad = [cam.distill_topk_backward(z, idx, val, o["stats"], g, temperature=T, tail=tail) for o, tail in zip(kd, (False, True))]
+    torch.cuda.synchronize()
+    want = -math.log(left) if T > 1 else 0.0
+    tol = (vocab / 128 + 40 + 8 + 16) * U * 2
+    assert float((out["logprob"].double() - want).abs().max()) <= tol and float((out["entropy"].double() + want).abs().max()) <= 16 * tol
+    assert bool((out["top_idx"][:, 0] == 100).all())
+    for x in (grad, *kd_grad):
+        assert bool(torch.isfinite(x).all()) and not bool(x[z == -math.inf].any())
+    if T > 1:
+        assert float((kd[0]["loss"].double() - (math.log(left) - math.log(3.0))).abs().max()) <= 2 * tol
+        assert float((kd[1]["loss"].double() - (math.log(left) - math.log(4.0) - 0.25 * math.log(left - 3.0))).abs().max()) <= 2 * tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset", [0.0, 1e4, -1e6, 1e7])
+@pytest.mark.parametrize("n,vocab", SHAPES)
+def test_renormalised_teacher_far_from_zero(cam, n, vocab, offset, dtype):
+    """The teacher's values shifted by a constant (whole numbers, so that the shift is exact) are the same distribution: the same loss
+    and gradient.  q_j is off by 4 u per unit of its exponent, at most 36 here, and k / 64 + 6 additions and 16 u for exp and the norm."""
+    k, T = 100, 0.5
+    z = rows_of(n, vocab, dtype, 10)
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    idx = torch.stack([torch.randperm(vocab, generator=gen, device="cuda")[:k] for _ in range(8)]).repeat(-(-n // 8), 1)[:n].int()
+    value = torch.randint(-9, 10, (n, k), generator=gen, device="cuda").float()
+    g = torch.linspace(0.5, 2.0, n, device="cuda")
+    out = cam.distill_topk(z, idx, value + offset, temperature=T)
+    got = cam.distill_topk_backward(z, idx, value + offset, out["stats"], g, temperature=T)
+    torch.cuda.synchronize()
+    log_q = torch.log_softmax(value.double() / T, 1)
+    q = log_q.exp()
+    lp = torch.log_softmax(z.double() / T, 1)
+    here = lp.gather(1, idx.long())
+    loss = (q * (log_q - here)).sum(1)
+    L = vocab / 128 + 40
+    assert bool(((out["loss"].double() - loss).abs() <= (4 * here.abs().amax(1) + L + 16) * U + U * loss.abs()).all())
+    dense = torch.zeros_like(lp).scatter_(1, idx.long(), q)
+    want = (lp.exp() - dense) * (g.double() / T)[:, None]
+    tol = (lp.exp() * (4 * lp.abs() + L + 16) * U + dense * (4 * 36 + 2 + 6 + 16) * U) * (g.double() / T)[:, None]
+    half = torch.finfo(TYPES[dtype]).eps / 2
+    bound = tol + half * (want.abs() + tol) + 2.0 ** -126
+    off = (got.double() - want).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
