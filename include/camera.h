@@ -399,8 +399,9 @@ int camera_output_error(camera_ctx* ctx, void* stream, const float* Y, const flo
  *   top_k    in [0, min(vocab, CAMERA_MAX_ALTERNATIVES)]; 0: top_idx and top_logprob are not written (may be NULL)
  *   logprob, entropy float32 [n], stats float32 [n x 2], top_idx int32 [n x top_k], top_logprob float32 [n x top_k] out; each of
  *            the first three may be NULL
- * Sums are taken in float32, in an order that depends on n, vocab and dtype only.  The workspace of a call serves every call with
- * the same or a smaller top_k, whatever n and vocab.  n == 0 does nothing.
+ * Sums are taken in float32, in an order that depends on n, vocab, dtype and on whether top_k is above 64 only (then many short rows
+ * are taken in larger workgroups).  The workspace of a call serves every call with the same or a smaller top_k, whatever n and vocab.
+ * n == 0 does nothing.
  *
  * camera_token_logprobs_backward: the gradient with respect to the logits of
  *   sum over i of grad_logprob[i] logprob[i] + grad_entropy[i] entropy[i]
