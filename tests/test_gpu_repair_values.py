@@ -223,7 +223,7 @@ def test_temperatures_at_the_ends(cam, n, vocab, T, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("offset", [0.0, 1e4, -1e6, 1e7])
+@pytest.mark.parametrize("offset", [0.0, -10.0, -20.0, 100.0, 1e4, -1e6, 1e7])
 @pytest.mark.parametrize("n,vocab", SHAPES)
 def test_renormalised_teacher_far_from_zero(cam, n, vocab, offset, dtype):
     """The teacher's values shifted by a constant (whole numbers, so that the shift is exact) are the same distribution: the same loss
