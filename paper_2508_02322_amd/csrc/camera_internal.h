@@ -340,9 +340,10 @@ hipError_t launch_sum_parts(hipStream_t stream, int dtype, const float* part, in
 hipError_t launch_zero(hipStream_t stream, void* dst, int64_t vectors);
 // H and / or pre of up to kGatedRowsMost tokens, bf16: every weight row is read once, straight into matrix operands.
 constexpr int kGatedRowsMost = 64;
-// Where that beats tiles: up to one tile of tokens always, beyond it while there is at most one workgroup of 16 channels a compute unit
-// (each reads every token again).  us, by rows / in tiles: 2560 x 3584, 64 tokens 24 / 36; 14336 x 4096, 16 tokens 48 / 47, 32
-// tokens 62 / 47, 64 tokens 99 / 47.
+// One tile of tokens always, more while there is at most one workgroup of 16 channels a compute unit (each reads every token again).
+// us, by rows / in tiles: 2560 x 3584, 1 token 10.4 / 20.5, 32 15.6 / 21.5, 64 23.4 / 21.9; 4096 x 4096, 1 12.8 / 23.1, 32 18.3 / 24.1,
+// 64 26.9 / 24.3.  Of wider blocks small tiles are as fast: 8192 x 4096, 1 token 23.4 / 23.1, 16 26.3 / 23.6; 20480 x 3584, 1 50 / 52,
+// 16 66 / 55; and at 14336 x 4096 faster: 1 41 / 35, 16 48 / 36.
 inline bool gated_by_rows(int64_t n, int64_t d_ff) { return n <= 16 || (n <= kGatedRowsMost && d_ff <= 16 * 256); }
 hipError_t launch_gated_rows(hipStream_t stream, const void* X, int64_t ldx, int64_t n, int64_t d_model, const void* W_gate,
                              const void* W_up, int64_t d_ff, void* H, int64_t ldh, float* pre, int64_t pre_ld);

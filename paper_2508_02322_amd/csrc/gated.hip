@@ -3,10 +3,12 @@
 // The three products dX = dG W_gate + dU W_up, dW_gate = dG^T X, dW_up = dU^T X run on the grouped contraction, whose operands are
 // both K-contiguous.  So dG and dU are written as rows (the left operand of dX, K = channels) and transposed (the left operands
 // of dW, K = tokens), and W_gate, W_up and X are transposed; the copies are padded with zeros to whole K tiles.
-// All of it is bound by memory.  8192 tokens, 20480 x 3584: the operands 860 us for 3.7 GB (4.3 TB/s; pieces of 128 bytes in rows
-// far apart: with tiles of 128 x 64 780 us, but 19 us instead of 14 where a block is small), the products 1.64 and 1.63 ms (1.46 and
-// 1.48 PFLOP/s), the forward product 1.65 ms, with the projections kept in float32 (1.34 GB more) 1.85.  Kept as bf16 they
-// would be half of that, and every gradient would carry two roundings more.
+// What this file does itself is bound by memory, the products by the matrix pipe.  8192 tokens, 20480 x 3584: the operands 857 us for
+// 3.7 GB (4.3 TB/s; pieces of 128 bytes in rows far apart: with tiles of 128 x 64 780 us, but 19 us instead of 14 where a block is
+// small), the products 1.63 and 1.59 ms (1.47 and 1.51 PFLOP/s), the forward product 1.66 ms, with the projections kept in float32
+// (1.34 GB more) 1.85, between the others 1.91.  Kept as bf16 they would be half of that, and every gradient would carry two roundings more.
+// bf16: dG and dU are rounded, half a step, because the matrix instructions take no wider operand: gradients are 0.0023 off in the
+// 2-norm where the final rounding alone makes 0.0017.  As a sum of two bf16 each they would not be, in twice the K of every product.
 #include <algorithm>
 
 #include "camera_internal.h"
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(uint4* __restrict__ dst,
 // operands of kSteps matrix instructions of K = 32 before it multiplies.  Lane 16 q + r holds K elements [8 q, 8 q + 8) of row r:
 // the weights are the left operand (16 channels), the tokens the right one (NT tiles of 16).  The waves' partial sums meet in LDS
 // and are added in wave order.  One token: 2560 x 3584 10.3 us (3.6 TB/s, 160 workgroups, all of their loads in flight at once),
-// 14336 x 4096 41 us (5.7 TB/s).
+// 14336 x 4096 41 us (5.7 TB/s; small tiles 35).
 constexpr int kRowsWaves = 8;
 constexpr int kChannels = 16;
 

@@ -106,8 +106,8 @@ constexpr int kChunkM = 4;     // otherwise this many
 //                 [row][column] and [column + col_gap] (if there is one); columns up to the next multiple of pad_hidden are written too
 //   kEpiRounded : kEpiProduct in the inputs' type -> rounded, the rows of expert e expert_gap elements further on for each e
 //   kEpiPart    : kEpiProduct, the K extent in ep.k_parts parts
-// (kEpiGated at 8192 tokens, 20480 x 3584: 1.65 ms, 1.85 with the projections, whose 1.34 GB are written behind the K loops with the
-// unit's only workgroup; kEpiRounded at the same sizes 1.64 ms, 1.46 PFLOP/s.)
+// (kEpiGated at 8192 tokens, 20480 x 3584: 1.66 ms, 1.85 with the projections, whose 1.34 GB are written behind the K loops with the
+// unit's only workgroup, and 1.91 within a training step; kEpiRounded at the same sizes 1.63 and 1.59 ms, 1.47 and 1.51 PFLOP/s.)
 enum { kEpiStats = 0, kEpiHidden = 1, kEpiProduct = 2, kEpiListed = 3, kEpiGated = 4, kEpiRounded = 5, kEpiPart = 6 };
 constexpr bool epi_hidden(int epi) { return epi == kEpiHidden || epi == kEpiListed; }
 constexpr bool epi_by_slot(int epi) { return epi == kEpiProduct || epi == kEpiRounded || epi == kEpiPart; }  // token rows = bucket slots

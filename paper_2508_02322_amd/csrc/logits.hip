@@ -9,9 +9,10 @@
 // difference of two infinities, stays in the sums and makes the row's results NaN; only the maxima pass it over.
 //
 // All of it is bound by reading the logits once (and writing the gradient once).  bf16, 4096 rows of 151936: log probabilities, entropy and
-// 64 alternatives 228 us (5.5 TB/s), distillation with 64 listed tokens and the rest as a class 217 us (5.8), gradients of 2048 rows
-// 224 us (5.6 read and written; a copy of as many bytes 4.9).  One row: 8.5 us in 33 parts and 6.3 us to join them, latencies: what
-// a part does after its one load (three reductions, the bound, the candidates) is a chain of LDS and cache round trips.
+// 64 alternatives 227 us (5.5 TB/s), distillation with 64 listed tokens and the rest as a class 214 us (5.8), gradients of 2048 rows
+// 223 us (5.6 read and written; a copy of as many bytes 4.9).  (After 20 ms of them; the first 10 ms of passes are a sixth slower.)
+// One row: 8.3 us in 33 parts and 6.5 us to join them, latencies: what a part does after its one load (three reductions, the bound, the
+// candidates) is a chain of LDS and cache round trips.
 #include <math.h>
 
 #include <algorithm>
@@ -320,8 +321,9 @@ struct ListKeys {
 // keys are all different, so the order in which candidates are found does not show.  Where more values reach the bound than there
 // is room for, they are mostly equal (a mask by the type's lowest value with fewer tokens left than wanted, a constant row): then
 // the larger values are taken and of the equal ones the first, in index order, one pass and the beginning of another.  Otherwise
-// the k-th largest key is found by its digits, eight passes over the source.  1024 x 102400 bf16, 5 tokens left, 20 alternatives: 101 us,
-// 745 by digits, 42 without ties.  4096 x 151936 bf16, us: 237 without alternatives, 228 to 231 with up to 64, 281 with 256 (half the lines again).
+// the k-th largest key is found by its digits, eight passes over the source.  1024 x 102400 bf16, 5 tokens left, 20 alternatives: 95 us,
+// 745 by digits, 42 without ties.  4096 x 151936 bf16, us: 216 without alternatives, 220 with one, 223 with 20, 227 with 64, 242 with 128,
+// 280 with 256 (half the lines again).
 template <int TH, class SOURCE, class OUT>
 __device__ __forceinline__ void select_top(const SOURCE& src, uint32_t largest, int k, SelectSmem<TH>& sm, OUT&& out) {
   constexpr int kWaves = TH / kWave, kCandidates = SelectSmem<TH>::kCandidates, kChosen = SelectSmem<TH>::kChosen;
@@ -987,8 +989,7 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // Parts of a row: as many as give the chip kLogitParts workgroups, each with at least a vector for every thread.  Many short rows
 // are left whole, in short workgroups, which the chip holds four times as many of.  us in long / short ones, 4096 rows, 20
-// alternatives: of 1000 33 / 15, of 4000 35 / 19, of 16000 46 / 37; of 32000 (beyond the line) 59 in long ones, where the copy of as
-// many bytes takes 53.
+// alternatives: of 1000 31 / 13, of 4000 32 / 17, of 16000 43 / 36; of 32000 (beyond the line) 54 in long ones.
 LogitPlan logit_plan(int dtype, int64_t n, int64_t vocab, bool marks, int top_k) {
   const int64_t vec = dtype == CAMERA_BF16 ? 8 : 4, least = kLong * vec;
   LogitPlan plan{1, vocab, kShort};
