@@ -88,3 +88,34 @@ def test_a_model_is_no_distance_from_itself(cam, tail):
         reach = float(teacher.logprob.abs().max())
         assert float(out.kl.abs().max()) < 4 * (4 * reach + 3001 / 512 + 48) * U
         assert float(out.dlogits.abs().max()) < 4 * (4 * reach + 3001 / 512 + 48) * U * max(1.0, 1 / T)
+
+
+def test_renormalised_step_in_a_graph(cam):
+    """Captured once at a temperature of its own and replayed after the logits and the teacher changed, in turn with eager calls."""
+    n, vocab, T = 33, 2003, 2.0
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    logits = torch.randn((n, vocab), generator=gen, device="cuda").to(torch.bfloat16)
+    teacher = pipeline.teacher_of(cam, torch.randn((n, vocab), generator=gen, device="cuda").to(torch.bfloat16), 8, T)
+    targets = torch.randint(0, vocab, (n,), generator=gen, device="cuda").int()
+    g = torch.ones(n, device="cuda")
+
+    def step():
+        out = pipeline.recovery_step(cam, logits, targets, teacher, g, g, tail=False)
+        return out.logprob, out.entropy, out.kl, out.dlogits
+    step()
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            captured = step()
+    for trial in range(4):
+        if trial:
+            logits.copy_(torch.randn(logits.shape, generator=gen, device="cuda"))
+            teacher.logprob.copy_(-3 * torch.rand(teacher.logprob.shape, generator=gen, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in captured]
+        for a, b in zip(kept, step()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
